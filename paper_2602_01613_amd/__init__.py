@@ -35,3 +35,16 @@ from .binding import (  # noqa: F401
     TN_QUERY_NUM_STEPS, TN_QUERY_CHUNK_TOKENS, TN_QUERY_MAX_INTERMEDIATE, TN_QUERY_OUT_FEATURES,
     TN_QUERY_IN_FEATURES, TN_QUERY_NUM_MERGES, TN_QUERY_STEP_BASE,
 )
+from .fp8 import (  # noqa: F401
+    FP8_EXPORTED_SYMBOLS,
+    Fp8Linear,
+    Fp8Rows,
+    RowOutput,
+    TN_DTYPE_FP8,
+    TN_FP8_BLOCK,
+    quantize_fp8,
+    rms_norm,
+    rms_norm_gradients,
+    silu_gate,
+    silu_gate_gradients,
+)

@@ -1,0 +1,413 @@
+// The operators around 8-bit projections (include/tn_fp8.h): host side and C ABI. Kernels: kernels/fp8_*.hpp.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <new>
+
+#include "../../include/tn_fp8.h"
+
+namespace {
+
+#include "kernels/fp8_format.hpp"
+#include "kernels/fp8_norm.hpp"
+#include "kernels/fp8_rows.hpp"
+#include "kernels/fp8_weight.hpp"
+#include "kernels/fp8_stream.hpp"
+
+constexpr int64_t kMaxRows = int64_t(1) << 30;
+constexpr int64_t kMaxCols = int64_t(1) << 24;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? TN_OK : TN_ERR_HIP; }
+int64_t element_bytes(int32_t dtype) { return dtype == TN_DTYPE_F32 ? 4 : 2; }
+
+RowLayout row_layout(int64_t cols, int32_t segments) {
+    RowLayout l;
+    l.blocks = int32_t(div_up(cols, kBlock));
+    l.code_stride = int64_t(segments) * l.blocks * kBlock;
+    l.scale_stride = div_up(int64_t(segments) * l.blocks, 4) * 4;
+    l.spare = int32_t(l.scale_stride - int64_t(segments) * l.blocks);
+    return l;
+}
+
+bool sizes_fit(int64_t rows, int64_t cols) { return rows <= kMaxRows && cols <= kMaxCols; }
+// a matrix the caller gives: there, its rows apart, its elements aligned
+bool matrix_ok(const void* p, int64_t stride, int64_t cols, int32_t dtype) { return p && stride >= cols && aligned(p, unsigned(element_bytes(dtype))); }
+bool eight_bit_ok(const void* codes, const void* scales) {
+    return (!codes && !scales) || (codes && scales && aligned(codes, 16) && aligned(scales, 4));
+}
+bool float_type(int32_t dtype) { return dtype == TN_DTYPE_F32 || dtype == TN_DTYPE_BF16; }
+
+// ---------------------------------------------------------------------------------------------
+// norm
+// ---------------------------------------------------------------------------------------------
+// Waves to a row and chunks to a lane: `chunks` of 8 elements have to fit WAVES * 64 * NC.
+template <typename T, int WAVES, int NC>
+int run_norm(const NormArgs& a, hipStream_t stream) {
+    const int64_t groups = WAVES == 1 ? div_up(a.rows, 4) : a.rows;
+    rms_norm_kernel<T, WAVES, NC><<<dim3(unsigned(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, stream>>>(a);
+    return launched();
+}
+template <typename T>
+int dispatch_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
+    if (chunks <= 64) return run_norm<T, 1, 1>(a, stream);
+    if (chunks <= 256) return run_norm<T, 4, 1>(a, stream);
+    if (chunks <= 512) return run_norm<T, 4, 2>(a, stream);
+    if (chunks <= 768) return run_norm<T, 4, 3>(a, stream);
+    if (chunks <= 1024) return run_norm<T, 4, 4>(a, stream);
+    return run_norm<T, 16, 2>(a, stream);
+}
+
+int64_t norm_grad_groups(int64_t rows) { return rows < 512 ? rows : 512; }
+
+template <typename T, int WAVES, int NC>
+int run_norm_grad(const NormGradArgs& a, int64_t groups, hipStream_t stream) {
+    norm_grad_kernel<T, WAVES, NC><<<dim3(unsigned(groups)), dim3(WAVES * 64), 0, stream>>>(a);
+    return launched();
+}
+template <typename T>
+int dispatch_norm_grad(const NormGradArgs& a, int64_t chunks, int64_t groups, hipStream_t stream) {
+    if (chunks <= 64) return run_norm_grad<T, 1, 1>(a, groups, stream);
+    if (chunks <= 256) return run_norm_grad<T, 4, 1>(a, groups, stream);
+    if (chunks <= 512) return run_norm_grad<T, 4, 2>(a, groups, stream);
+    if (chunks <= 768) return run_norm_grad<T, 4, 3>(a, groups, stream);
+    if (chunks <= 1024) return run_norm_grad<T, 4, 4>(a, groups, stream);
+    return run_norm_grad<T, 16, 2>(a, groups, stream);
+}
+
+template <int OP>
+int run_rows(int32_t dtype, int64_t rows, const RowArgs& a, hipStream_t stream) {
+    if (rows == 0) return TN_OK;
+    const int64_t groups = div_up(a.items, 256);
+    if (groups > INT32_MAX) return TN_ERR_UNSUPPORTED;
+    if (dtype == TN_DTYPE_F32) row_kernel<float, OP><<<dim3(unsigned(groups)), dim3(256), 0, stream>>>(a);
+    else row_kernel<bf16_t, OP><<<dim3(unsigned(groups)), dim3(256), 0, stream>>>(a);
+    return launched();
+}
+
+}  // namespace
+
+struct tn_fp8_linear_s {
+    int32_t tensors = 1, transpose = 0;
+    int64_t m = 0, n = 0;                 // of each tensor
+    int32_t features = 0, f_blocks = 0;   // outputs of one of `out_segments` runs of features
+    int32_t out_segments = 1;
+    int32_t k_cols = 0, k_segments = 1;   // inputs: segments of k_cols
+    int32_t k_blocks = 0, scale_stride = 0;
+    unsigned char *packed = nullptr, *scales = nullptr;
+    int64_t packed_bytes = 0, scale_bytes = 0;
+    ~tn_fp8_linear_s() {
+        if (packed) (void)hipFree(packed);
+        if (scales) (void)hipFree(scales);
+    }
+};
+
+namespace {
+
+WeightArgs weight_args(const tn_fp8_linear_s& h, int slot) {
+    WeightArgs a{};
+    a.packed = h.packed;
+    a.scales = h.scales;
+    a.m = h.m;
+    a.n = h.n;
+    a.transpose = h.transpose;
+    a.k_blocks = h.k_blocks;
+    a.scale_stride = h.scale_stride;
+    const int m_blocks = int(div_up(h.m, kBlock));
+    a.f_block0 = h.transpose ? 0 : slot * m_blocks;
+    a.k_block0 = h.transpose ? slot * m_blocks : 0;
+    return a;
+}
+
+LinearArgs linear_args(const tn_fp8_linear_s& h, const void* codes, const void* scales, int64_t tokens) {
+    LinearArgs a{};
+    const RowLayout in = row_layout(h.k_cols, h.k_segments);
+    a.codes = static_cast<const unsigned char*>(codes);
+    a.scales = static_cast<const unsigned char*>(scales);
+    a.packed = h.packed;
+    a.w_scales = h.scales;
+    a.tokens = tokens;
+    a.code_stride = in.code_stride;
+    a.scale_stride = in.scale_stride;
+    a.k_blocks = h.k_blocks;
+    a.w_scale_stride = h.scale_stride;
+    a.features = h.features;
+    a.f_pieces = h.f_blocks * 8;
+    a.tensors = h.out_segments;
+    return a;
+}
+
+template <int NT>
+int run_stream(const LinearArgs& a, hipStream_t stream) {
+    const dim3 grid(unsigned(a.f_pieces * a.tensors), unsigned(div_up(a.tokens, 16 * NT)));
+    stream_kernel<8, 1, NT><<<grid, dim3(512), 0, stream>>>(a);
+    return launched();
+}
+template <int NT>
+int run_stream_gated(const LinearArgs& a, hipStream_t stream) {
+    const dim3 grid(unsigned(a.f_pieces / 8), unsigned(div_up(a.tokens, 16 * NT)));
+    stream_gated_kernel<NT><<<grid, dim3(1024), 0, stream>>>(a);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int tn_fp8_row_strides(int64_t cols, int32_t segments, int64_t* code_stride, int64_t* scale_stride) {
+    if (cols < 1 || segments < 1) return TN_ERR_INVALID_ARG;
+    if (cols > kMaxCols || segments > 256) return TN_ERR_UNSUPPORTED;
+    const RowLayout l = row_layout(cols, segments);
+    if (code_stride) *code_stride = l.code_stride;
+    if (scale_stride) *scale_stride = l.scale_stride;
+    return TN_OK;
+}
+
+int tn_fp8_quantize(int32_t dtype, int64_t rows, int64_t cols, int32_t segments, const void* x, int64_t x_stride,
+                    void* codes, void* scales, void* stream) {
+    if (!float_type(dtype) || rows < 0 || cols < 1 || segments < 1) return TN_ERR_INVALID_ARG;
+    if (!sizes_fit(rows, cols) || segments > 256) return TN_ERR_UNSUPPORTED;
+    if (rows == 0) return TN_OK;
+    if (!matrix_ok(x, x_stride, cols * segments, dtype) || !codes || !eight_bit_ok(codes, scales)) return TN_ERR_INVALID_ARG;
+    RowArgs a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.codes = static_cast<unsigned char*>(codes);
+    a.scales = static_cast<unsigned char*>(scales);
+    a.out = row_layout(cols, segments);
+    a.cols = int32_t(cols);
+    a.segments = segments;
+    a.per_row = int32_t(a.out.code_stride / kChunk);
+    a.items = rows * a.per_row;
+    return run_rows<ROW_QUANTIZE>(dtype, rows, a, static_cast<hipStream_t>(stream));
+}
+
+int tn_rms_norm(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t x_stride, const void* residual,
+                int64_t residual_stride, const void* weight, float eps, void* sum, int64_t sum_stride, void* y,
+                int64_t y_stride, void* codes, void* scales, void* stream) {
+    if (!float_type(dtype) || rows < 0 || cols < 1 || !(eps >= 0.f)) return TN_ERR_INVALID_ARG;
+    if (rows > kMaxRows || cols > TN_FP8_MAX_NORM_COLS) return TN_ERR_UNSUPPORTED;
+    if (rows == 0) return TN_OK;
+    if (!sum && !y && !codes) return TN_ERR_INVALID_ARG;
+    if (!matrix_ok(x, x_stride, cols, dtype) || (residual && !matrix_ok(residual, residual_stride, cols, dtype)) ||
+        (sum && !matrix_ok(sum, sum_stride, cols, dtype)) || (y && !matrix_ok(y, y_stride, cols, dtype)) ||
+        !aligned(weight, unsigned(element_bytes(dtype))) || !eight_bit_ok(codes, scales))
+        return TN_ERR_INVALID_ARG;
+    NormArgs a{};
+    a.x = x;
+    a.residual = residual;
+    a.weight = weight;
+    a.sum = sum;
+    a.y = y;
+    a.codes = static_cast<unsigned char*>(codes);
+    a.scales = static_cast<unsigned char*>(scales);
+    a.rows = rows;
+    a.x_stride = x_stride;
+    a.residual_stride = residual_stride;
+    a.sum_stride = sum_stride;
+    a.y_stride = y_stride;
+    a.out = row_layout(cols, 1);
+    a.cols = int32_t(cols);
+    a.eps = eps;
+    const int64_t chunks = codes ? a.out.code_stride / kChunk : div_up(cols, kChunk);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return dtype == TN_DTYPE_F32 ? dispatch_norm<float>(a, chunks, st) : dispatch_norm<bf16_t>(a, chunks, st);
+}
+
+int64_t tn_rms_norm_gradients_workspace(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 1) return TN_ERR_INVALID_ARG;
+    if (rows > kMaxRows || cols > TN_FP8_MAX_NORM_COLS) return TN_ERR_UNSUPPORTED;
+    return norm_grad_groups(rows) * cols * 4;
+}
+
+int tn_rms_norm_gradients(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t dy_stride, const void* s,
+                          int64_t s_stride, const void* weight, float eps, const void* dsum, int64_t dsum_stride, void* dx,
+                          int64_t dx_stride, float* dweight, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!float_type(dtype) || rows < 0 || cols < 1 || !(eps >= 0.f)) return TN_ERR_INVALID_ARG;
+    const int64_t need = tn_rms_norm_gradients_workspace(rows, cols);
+    if (need < 0) return int(need);
+    if (!aligned(dweight, 4) || (dweight && need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))) return TN_ERR_INVALID_ARG;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t groups = norm_grad_groups(rows);
+    if (rows > 0) {
+        if (!matrix_ok(dy, dy_stride, cols, dtype) || !matrix_ok(s, s_stride, cols, dtype) || !matrix_ok(dx, dx_stride, cols, dtype) ||
+            (dsum && !matrix_ok(dsum, dsum_stride, cols, dtype)) || !aligned(weight, unsigned(element_bytes(dtype))))
+            return TN_ERR_INVALID_ARG;
+        NormGradArgs a{};
+        a.dy = dy;
+        a.s = s;
+        a.weight = weight;
+        a.dsum = dsum;
+        a.dx = dx;
+        a.partial = dweight ? static_cast<float*>(workspace) : nullptr;
+        a.rows = rows;
+        a.dy_stride = dy_stride;
+        a.s_stride = s_stride;
+        a.dsum_stride = dsum_stride;
+        a.dx_stride = dx_stride;
+        a.cols = int32_t(cols);
+        a.eps = eps;
+        const int64_t chunks = div_up(cols, kChunk);
+        const int rc = dtype == TN_DTYPE_F32 ? dispatch_norm_grad<float>(a, chunks, groups, st) : dispatch_norm_grad<bf16_t>(a, chunks, groups, st);
+        if (rc != TN_OK) return rc;
+    }
+    if (!dweight) return TN_OK;
+    norm_grad_reduce_kernel<<<dim3(unsigned(div_up(cols, 64))), dim3(1024), 0, st>>>(static_cast<const float*>(workspace), int(groups), int(cols), dweight);
+    return launched();
+}
+
+int tn_silu_gate(int32_t dtype, int64_t rows, int64_t cols, const void* gate_up, int64_t gate_up_stride, void* y,
+                 int64_t y_stride, void* codes, void* scales, void* stream) {
+    if (!float_type(dtype) || rows < 0 || cols < 1) return TN_ERR_INVALID_ARG;
+    if (!sizes_fit(rows, cols)) return TN_ERR_UNSUPPORTED;
+    if (rows == 0) return TN_OK;
+    if ((!y && !codes) || !matrix_ok(gate_up, gate_up_stride, 2 * cols, dtype) || (y && !matrix_ok(y, y_stride, cols, dtype)) || !eight_bit_ok(codes, scales))
+        return TN_ERR_INVALID_ARG;
+    RowArgs a{};
+    a.x = gate_up;
+    a.x_stride = gate_up_stride;
+    a.y = y;
+    a.y_stride = y_stride;
+    a.codes = static_cast<unsigned char*>(codes);
+    a.scales = static_cast<unsigned char*>(scales);
+    a.out = row_layout(cols, 1);
+    a.cols = int32_t(cols);
+    a.segments = 1;
+    a.per_row = a.out.blocks * (kBlock / kChunk);
+    a.items = rows * a.per_row;
+    return run_rows<ROW_GATE>(dtype, rows, a, static_cast<hipStream_t>(stream));
+}
+
+int tn_silu_gate_gradients(int32_t dtype, int64_t rows, int64_t cols, const void* gate_up, int64_t gate_up_stride,
+                           const void* dh, int64_t dh_stride, void* d_gate_up, int64_t d_gate_up_stride, void* codes,
+                           void* scales, void* stream) {
+    if (!float_type(dtype) || rows < 0 || cols < 1) return TN_ERR_INVALID_ARG;
+    if (!sizes_fit(rows, cols)) return TN_ERR_UNSUPPORTED;
+    if (rows == 0) return TN_OK;
+    if ((!d_gate_up && !codes) || !matrix_ok(gate_up, gate_up_stride, 2 * cols, dtype) || !matrix_ok(dh, dh_stride, cols, dtype) ||
+        (d_gate_up && !matrix_ok(d_gate_up, d_gate_up_stride, 2 * cols, dtype)) || !eight_bit_ok(codes, scales))
+        return TN_ERR_INVALID_ARG;
+    RowArgs a{};
+    a.x = gate_up;
+    a.x_stride = gate_up_stride;
+    a.dh = dh;
+    a.dh_stride = dh_stride;
+    a.y = d_gate_up;
+    a.y_stride = d_gate_up_stride;
+    a.codes = static_cast<unsigned char*>(codes);
+    a.scales = static_cast<unsigned char*>(scales);
+    a.out = row_layout(cols, 2);
+    a.cols = int32_t(cols);
+    a.segments = 2;
+    a.per_row = a.out.blocks * (kBlock / kChunk);
+    a.items = rows * a.per_row;
+    return run_rows<ROW_GATE_GRAD>(dtype, rows, a, static_cast<hipStream_t>(stream));
+}
+
+int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
+    if (!out || !d || !d->tensors || d->out_features < 1 || d->in_features < 1 || d->max_tokens < 1) return TN_ERR_INVALID_ARG;
+    const bool given = d->dtype == TN_DTYPE_FP8;
+    if ((!given && !float_type(d->dtype)) || (given && !d->scales) || d->n_tensors < 1 || d->n_tensors > 2 || (d->flags & ~TN_FLAG_TRANSPOSE))
+        return TN_ERR_INVALID_ARG;
+    if (d->out_features > TN_FP8_MAX_FEATURES || d->in_features > TN_FP8_MAX_FEATURES || d->max_tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    for (int i = 0; i < d->n_tensors; ++i)
+        if (!d->tensors[i] || (given && !d->scales[i]) || (!given && !aligned(d->tensors[i], unsigned(element_bytes(d->dtype))))) return TN_ERR_INVALID_ARG;
+    tn_fp8_linear_s* h = new (std::nothrow) tn_fp8_linear_s;
+    if (!h) return TN_ERR_ALLOC;
+    h->tensors = d->n_tensors;
+    h->transpose = (d->flags & TN_FLAG_TRANSPOSE) ? 1 : 0;
+    h->m = d->out_features;
+    h->n = d->in_features;
+    h->features = int32_t(h->transpose ? h->n : h->m);
+    h->f_blocks = int32_t(div_up(h->features, kBlock));
+    h->out_segments = h->transpose ? 1 : h->tensors;
+    h->k_cols = int32_t(h->transpose ? h->m : h->n);
+    h->k_segments = h->transpose ? h->tensors : 1;
+    h->k_blocks = int32_t(h->k_segments * div_up(h->k_cols, kBlock));
+    h->scale_stride = int32_t(div_up(h->k_blocks, 4) * 4);
+    h->packed_bytes = int64_t(h->out_segments) * h->f_blocks * 8 * h->k_blocks * 2048;
+    h->scale_bytes = int64_t(h->out_segments) * h->f_blocks * h->scale_stride;
+    const hipStream_t st = static_cast<hipStream_t>(d->stream);
+    int rc = TN_OK;
+    if (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
+        hipMalloc(reinterpret_cast<void**>(&h->scales), size_t(h->scale_bytes)) != hipSuccess) {
+        (void)hipGetLastError();
+        rc = TN_ERR_ALLOC;
+    }
+    for (int i = 0; rc == TN_OK && i < h->tensors; ++i) {
+        WeightArgs a = weight_args(*h, i);
+        a.src = d->tensors[i];
+        a.src_scales = given ? static_cast<const unsigned char*>(d->scales[i]) : nullptr;
+        const dim3 grid(unsigned(div_up(h->n, kBlock)), unsigned(div_up(h->m, kBlock)));
+        if (given) weight_pack_kernel<unsigned char><<<grid, dim3(256), 0, st>>>(a);
+        else if (d->dtype == TN_DTYPE_F32) weight_pack_kernel<float><<<grid, dim3(256), 0, st>>>(a);
+        else weight_pack_kernel<bf16_t><<<grid, dim3(256), 0, st>>>(a);
+        rc = launched();
+    }
+    if (rc == TN_OK && hipStreamSynchronize(st) != hipSuccess) rc = TN_ERR_HIP;
+    if (rc != TN_OK) {
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return TN_OK;
+}
+
+int tn_fp8_linear_forward(tn_fp8_linear_t h, const void* codes, const void* scales, void* y, int64_t y_stride, int64_t tokens, void* stream) {
+    if (!h || tokens < 0) return TN_ERR_INVALID_ARG;
+    if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    if (tokens == 0) return TN_OK;
+    if (!codes || !eight_bit_ok(codes, scales) || !matrix_ok(y, y_stride, int64_t(h->out_segments) * h->features, TN_DTYPE_BF16)) return TN_ERR_INVALID_ARG;
+    LinearArgs a = linear_args(*h, codes, scales, tokens);
+    a.y = y;
+    a.y_stride = y_stride;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (div_up(tokens, 64) > 65535) return TN_ERR_UNSUPPORTED;
+    return tokens <= 16 ? run_stream<1>(a, st) : run_stream<4>(a, st);
+}
+
+int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales, void* out_codes, void* out_scales, int64_t tokens, void* stream) {
+    if (!h || tokens < 0 || h->out_segments != 2) return TN_ERR_INVALID_ARG;
+    if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    if (tokens == 0) return TN_OK;
+    if (!codes || !out_codes || !eight_bit_ok(codes, scales) || !eight_bit_ok(out_codes, out_scales)) return TN_ERR_INVALID_ARG;
+    LinearArgs a = linear_args(*h, codes, scales, tokens);
+    const RowLayout o = row_layout(h->features, 1);
+    a.out_codes = static_cast<unsigned char*>(out_codes);
+    a.out_scales = static_cast<unsigned char*>(out_scales);
+    a.out_code_stride = o.code_stride;
+    a.out_scale_stride = o.scale_stride;
+    a.spare = o.spare;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (div_up(tokens, 32) > 65535) return TN_ERR_UNSUPPORTED;
+    return tokens <= 16 ? run_stream_gated<1>(a, st) : run_stream_gated<2>(a, st);
+}
+
+int tn_fp8_linear_tensor(tn_fp8_linear_t h, int32_t slot, void* codes, void* scales, void* stream) {
+    if (!h || slot < 0 || slot >= h->tensors) return TN_ERR_INVALID_ARG;
+    if (!codes && !scales) return TN_OK;
+    const dim3 grid(unsigned(div_up(h->n, kBlock)), unsigned(div_up(h->m, kBlock)));
+    weight_unpack_kernel<<<grid, dim3(256), 0, static_cast<hipStream_t>(stream)>>>(weight_args(*h, slot), static_cast<unsigned char*>(codes),
+                                                                                   static_cast<unsigned char*>(scales));
+    return launched();
+}
+
+int tn_fp8_linear_query(tn_fp8_linear_t h, int32_t what, int64_t* value) {
+    if (!h || !value) return TN_ERR_INVALID_ARG;
+    switch (what) {
+        case TN_QUERY_OUT_FEATURES: *value = int64_t(h->out_segments) * h->features; return TN_OK;
+        case TN_QUERY_IN_FEATURES: *value = int64_t(h->k_segments) * h->k_cols; return TN_OK;
+        case TN_QUERY_PARAM_COUNT: *value = h->tensors * h->m * h->n; return TN_OK;
+        case TN_QUERY_PACKED_BYTES: *value = h->packed_bytes + h->scale_bytes; return TN_OK;
+        case TN_QUERY_WORKSPACE_BYTES: *value = 0; return TN_OK;
+        default: return TN_ERR_INVALID_ARG;
+    }
+}
+
+int tn_fp8_linear_destroy(tn_fp8_linear_t h) {
+    delete h;
+    return TN_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,376 @@
+"""ctypes binding of the operators around 8-bit projections (include/tn_fp8.h): argument marshalling only.
+
+Root-mean-square norm with the residual's addition, silu(gate) * up, products of 8-bit weights with 8-bit activations, and
+the gradients of all three. Tensors are torch CUDA (ROCm) tensors; work goes to the current HIP stream. Nothing here computes.
+
+    layer = tn.Fp8Linear([w_gate, w_up], max_tokens=8192)        # bf16 or fp32 [M, N] weights, quantised at create
+    n = tn.rms_norm(x, weight, residual=res, outputs="fp8")      # n.sum = x + res, n.fp8 = the norm in 8 bits
+    h = layer.gated(n.fp8)                                       # silu(gate) * up in 8 bits
+    y = down(h)                                                  # bf16
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import List, NamedTuple, Optional, Sequence, Tuple
+
+import torch
+
+from .binding import (TN_DTYPE_BF16, TN_DTYPE_F32, TN_FLAG_TRANSPOSE, TN_QUERY_IN_FEATURES, TN_QUERY_OUT_FEATURES, TNLinearError,
+                      load_library)
+
+TN_DTYPE_FP8 = 2
+TN_FP8_BLOCK = 128
+
+FP8_EXPORTED_SYMBOLS = (
+    "tn_fp8_row_strides",
+    "tn_fp8_quantize",
+    "tn_rms_norm",
+    "tn_rms_norm_gradients",
+    "tn_rms_norm_gradients_workspace",
+    "tn_silu_gate",
+    "tn_silu_gate_gradients",
+    "tn_fp8_linear_create",
+    "tn_fp8_linear_forward",
+    "tn_fp8_linear_gated",
+    "tn_fp8_linear_tensor",
+    "tn_fp8_linear_query",
+    "tn_fp8_linear_destroy",
+)
+
+_CODES, _SCALES = torch.float8_e4m3fn, torch.float8_e8m0fnu
+_DTYPE = {torch.float32: TN_DTYPE_F32, torch.bfloat16: TN_DTYPE_BF16}
+
+
+class _Desc(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("n_tensors", ctypes.c_int32),
+        ("out_features", ctypes.c_int64),
+        ("in_features", ctypes.c_int64),
+        ("tensors", ctypes.POINTER(ctypes.c_void_p)),
+        ("scales", ctypes.POINTER(ctypes.c_void_p)),
+        ("max_tokens", ctypes.c_int64),
+        ("flags", ctypes.c_int32),
+        ("stream", ctypes.c_void_p),
+    ]
+
+
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = load_library()
+        p, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        args = {
+            "tn_fp8_row_strides": [i64, i32, ctypes.POINTER(i64), ctypes.POINTER(i64)],
+            "tn_fp8_quantize": [i32, i64, i64, i32, p, i64, p, p, p],
+            "tn_rms_norm": [i32, i64, i64, p, i64, p, i64, p, f32, p, i64, p, i64, p, p, p],
+            "tn_rms_norm_gradients": [i32, i64, i64, p, i64, p, i64, p, f32, p, i64, p, i64, p, p, i64, p],
+            "tn_rms_norm_gradients_workspace": [i64, i64],
+            "tn_silu_gate": [i32, i64, i64, p, i64, p, i64, p, p, p],
+            "tn_silu_gate_gradients": [i32, i64, i64, p, i64, p, i64, p, i64, p, p, p],
+            "tn_fp8_linear_create": [ctypes.POINTER(p), ctypes.POINTER(_Desc)],
+            "tn_fp8_linear_forward": [p, p, p, p, i64, i64, p],
+            "tn_fp8_linear_gated": [p, p, p, p, p, i64, p],
+            "tn_fp8_linear_tensor": [p, i32, p, p, p],
+            "tn_fp8_linear_query": [p, i32, ctypes.POINTER(i64)],
+            "tn_fp8_linear_destroy": [p],
+        }
+        for name, types in args.items():
+            fn = getattr(lib, name)
+            fn.argtypes = types
+            fn.restype = i64 if name == "tn_rms_norm_gradients_workspace" else ctypes.c_int
+        _lib = lib
+    return _lib
+
+
+def _check(status: int, where: str) -> None:
+    if status != 0:
+        raise TNLinearError(status, where)
+
+
+def _stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _matrix(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype) -> int:
+    """The row stride of t, a CUDA [rows, cols] matrix of dtype whose rows are contiguous and apart."""
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols):
+        raise ValueError(f"{name} must be a CUDA [{rows}, {cols}] tensor of {dtype}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    stride = t.stride(0) if rows > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or stride < cols:
+        raise ValueError(f"{name}: elements of a row must be contiguous and rows must not overlap (strides {t.stride()})")
+    return stride
+
+
+def _input(name: str, t: torch.Tensor) -> int:
+    """The type code of an input matrix that sets the type of a call."""
+    code = _DTYPE.get(t.dtype)
+    if code is None or t.dim() != 2 or t.shape[1] < 1 or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA [rows, cols] tensor of float32 or bfloat16, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return code
+
+
+def _vector(name: str, t: Optional[torch.Tensor], cols: int, dtype: torch.dtype) -> Optional[int]:
+    if t is None:
+        return None
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 1 and t.shape[0] == cols and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous CUDA [{cols}] tensor of {dtype}")
+    return t.data_ptr()
+
+
+class Fp8Rows:
+    """Rows in 8 bits: `codes` (float8_e4m3fn [rows, segments * P], P = cols rounded up to 128) and `scales` (float8_e8m0fnu
+    [rows, S], one for each block of 128, S rounded up to 4), as include/tn_fp8.h lays them out. `values` and `block_scales`
+    are views of a segment without its padding."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "segments")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, segments: int = 1):
+        width, blocks = -(-cols // TN_FP8_BLOCK) * TN_FP8_BLOCK * segments, -(-cols // TN_FP8_BLOCK) * segments
+        rows = codes.shape[0]
+        if not (codes.is_cuda and codes.dtype == _CODES and codes.is_contiguous() and tuple(codes.shape) == (rows, width)):
+            raise ValueError(f"codes must be a contiguous CUDA [rows, {width}] tensor of float8_e4m3fn")
+        if not (scales.is_cuda and scales.dtype == _SCALES and scales.is_contiguous() and tuple(scales.shape) == (rows, -(-blocks // 4) * 4)):
+            raise ValueError(f"scales must be a contiguous CUDA [{rows}, {-(-blocks // 4) * 4}] tensor of float8_e8m0fnu")
+        self.codes, self.scales, self.rows, self.cols, self.segments = codes, scales, rows, cols, segments
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, segments: int = 1, device="cuda") -> "Fp8Rows":
+        blocks = -(-cols // TN_FP8_BLOCK) * segments
+        new = cls.__new__(cls)
+        new.codes = torch.empty((rows, blocks * TN_FP8_BLOCK), dtype=_CODES, device=device)
+        new.scales = torch.empty((rows, -(-blocks // 4) * 4), dtype=_SCALES, device=device)
+        new.rows, new.cols, new.segments = rows, cols, segments
+        return new
+
+    def values(self, segment: int = 0) -> torch.Tensor:
+        start = segment * (-(-self.cols // TN_FP8_BLOCK) * TN_FP8_BLOCK)
+        return self.codes[:, start:start + self.cols]
+
+    def block_scales(self, segment: int = 0) -> torch.Tensor:
+        blocks = -(-self.cols // TN_FP8_BLOCK)
+        return self.scales[:, segment * blocks:(segment + 1) * blocks]
+
+    def _ready(self, name: str, rows: int, cols: int, segments: int) -> "Fp8Rows":
+        if (self.rows, self.cols, self.segments) != (rows, cols, segments):
+            raise ValueError(f"{name} holds [{self.rows}, {self.segments} x {self.cols}], not [{rows}, {segments} x {cols}]")
+        return self
+
+
+class RowOutput(NamedTuple):
+    """What a row operator returns; None for what was not asked for."""
+    y: Optional[torch.Tensor]
+    fp8: Optional[Fp8Rows]
+    sum: Optional[torch.Tensor] = None
+
+
+_OUTPUTS = {"y": (True, False), "fp8": (False, True), "both": (True, True)}
+
+
+def _outputs(outputs: str, out: Optional[RowOutput], like: torch.Tensor, rows: int, cols: int, segments: int):
+    """(y, fp8, row stride of y) of a call: the caller's, or new ones."""
+    if outputs not in _OUTPUTS:
+        raise ValueError('outputs is "y", "fp8" or "both"')
+    want_y, want_fp8 = _OUTPUTS[outputs]
+    y, fp8, stride = None, None, 0
+    if want_y:
+        y = out.y if out is not None and out.y is not None else torch.empty((rows, segments * cols), dtype=like.dtype, device=like.device)
+        stride = _matrix("out.y", y, rows, segments * cols, like.dtype)
+    if want_fp8:
+        fp8 = out.fp8._ready("out.fp8", rows, cols, segments) if out is not None and out.fp8 is not None else Fp8Rows.empty(rows, cols, segments, like.device)
+    return y, fp8, stride
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def quantize_fp8(x: torch.Tensor, segments: int = 1, out: Optional[Fp8Rows] = None) -> Fp8Rows:
+    """x [rows, segments * cols] in 8 bits, each segment in blocks of its own."""
+    code = _input("x", x)
+    rows, width = x.shape
+    if segments < 1 or width % segments:
+        raise ValueError(f"x has {width} columns: not {segments} equal segments")
+    cols = width // segments
+    stride = _matrix("x", x, rows, width, x.dtype)
+    out = Fp8Rows.empty(rows, cols, segments, x.device) if out is None else out._ready("out", rows, cols, segments)
+    _check(_library().tn_fp8_quantize(code, rows, cols, segments, x.data_ptr(), stride, out.codes.data_ptr(), out.scales.data_ptr(), _stream()),
+           "tn_fp8_quantize")
+    return out
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
+             outputs: str = "y", out: Optional[RowOutput] = None) -> RowOutput:
+    """s = x + residual (in x's type), y = s / sqrt(mean(s^2) + eps) * weight. `outputs`: "y" (x's type), "fp8" (8 bits) or
+    "both". Returns (y, fp8, sum); sum is s where there is a residual, and may be given as out.sum (x and residual
+    themselves too)."""
+    code = _input("x", x)
+    rows, cols = x.shape
+    x_stride = _matrix("x", x, rows, cols, x.dtype)
+    y, fp8, y_stride = _outputs(outputs, out, x, rows, cols, 1)
+    total, res_stride, sum_stride = None, 0, 0
+    if residual is not None:
+        res_stride = _matrix("residual", residual, rows, cols, x.dtype)
+        total = out.sum if out is not None and out.sum is not None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        sum_stride = _matrix("out.sum", total, rows, cols, x.dtype)
+    _check(_library().tn_rms_norm(code, rows, cols, x.data_ptr(), x_stride, _ptr(residual), res_stride, _vector("weight", weight, cols, x.dtype),
+                                  eps, _ptr(total), sum_stride, _ptr(y), y_stride, fp8.codes.data_ptr() if fp8 else None,
+                                  fp8.scales.data_ptr() if fp8 else None, _stream()), "tn_rms_norm")
+    return RowOutput(y, fp8, total)
+
+
+def rms_norm_gradients(dy: torch.Tensor, s: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                       dsum: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, dweight: bool = True
+                       ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(dx, dweight) of rms_norm for the gradient dy of its y and, where s is read elsewhere too, the gradient dsum that arrives
+    there: dx in s's type, for x and the residual alike; dweight in fp32 (None without a weight, or with dweight=False).
+    s is what rms_norm returned as sum (x, if it had no residual)."""
+    code = _input("s", s)
+    rows, cols = s.shape
+    s_stride = _matrix("s", s, rows, cols, s.dtype)
+    dy_stride = _matrix("dy", dy, rows, cols, s.dtype)
+    ds_stride = 0 if dsum is None else _matrix("dsum", dsum, rows, cols, s.dtype)
+    if dx is None:
+        dx = torch.empty((rows, cols), dtype=s.dtype, device=s.device)
+    dx_stride = _matrix("dx", dx, rows, cols, s.dtype)
+    lib = _library()
+    dw, space, need = None, None, 0
+    if dweight and weight is not None:
+        need = lib.tn_rms_norm_gradients_workspace(rows, cols)
+        if need < 0:
+            _check(int(need), "tn_rms_norm_gradients_workspace")
+        dw = torch.empty((cols,), dtype=torch.float32, device=s.device)
+        space = torch.empty((need,), dtype=torch.uint8, device=s.device)
+    _check(lib.tn_rms_norm_gradients(code, rows, cols, dy.data_ptr(), dy_stride, s.data_ptr(), s_stride, _vector("weight", weight, cols, s.dtype),
+                                     eps, _ptr(dsum), ds_stride, dx.data_ptr(), dx_stride, _ptr(dw), _ptr(space), need, _stream()),
+           "tn_rms_norm_gradients")
+    return dx, dw
+
+
+def silu_gate(gate_up: torch.Tensor, outputs: str = "y", out: Optional[RowOutput] = None) -> RowOutput:
+    """silu(gate) * up of gate_up = [gate | up], [rows, 2 * cols]; outputs as in rms_norm."""
+    code = _input("gate_up", gate_up)
+    rows, cols = gate_up.shape[0], gate_up.shape[1] // 2
+    stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype)
+    y, fp8, y_stride = _outputs(outputs, out, gate_up, rows, cols, 1)
+    _check(_library().tn_silu_gate(code, rows, cols, gate_up.data_ptr(), stride, _ptr(y), y_stride, fp8.codes.data_ptr() if fp8 else None,
+                                   fp8.scales.data_ptr() if fp8 else None, _stream()), "tn_silu_gate")
+    return RowOutput(y, fp8)
+
+
+def silu_gate_gradients(gate_up: torch.Tensor, dh: torch.Tensor, outputs: str = "y", out: Optional[RowOutput] = None) -> RowOutput:
+    """[dgate | dup] for the gradient dh of silu(gate) * up; in 8 bits they are two segments."""
+    code = _input("gate_up", gate_up)
+    rows, cols = gate_up.shape[0], gate_up.shape[1] // 2
+    stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype)
+    dh_stride = _matrix("dh", dh, rows, cols, gate_up.dtype)
+    y, fp8, y_stride = _outputs(outputs, out, gate_up, rows, cols, 2)
+    _check(_library().tn_silu_gate_gradients(code, rows, cols, gate_up.data_ptr(), stride, dh.data_ptr(), dh_stride, _ptr(y), y_stride,
+                                             fp8.codes.data_ptr() if fp8 else None, fp8.scales.data_ptr() if fp8 else None, _stream()),
+           "tn_silu_gate_gradients")
+    return RowOutput(y, fp8)
+
+
+class Fp8Linear:
+    """One 8-bit weight [M, N] living on the current GPU, or two that read the same activations (gate and up).
+
+    tensors  one or two contiguous CUDA tensors of float32 or bfloat16, quantised in blocks of 128 x 128; or, with `scales`,
+             float8_e4m3fn codes and their float8_e8m0fnu scales [ceil(M / 128), ceil(N / 128)]
+    transpose=True  the layer maps gradients of the outputs (two segments for two tensors) to that of the inputs
+    """
+
+    def __init__(self, tensors: Sequence[torch.Tensor], max_tokens: int, transpose: bool = False,
+                 scales: Optional[Sequence[torch.Tensor]] = None):
+        self._handle = None
+        if not torch.cuda.is_available():
+            raise RuntimeError("Fp8Linear needs a GPU: there is no CPU path")
+        tensors = list(tensors)
+        if len(tensors) not in (1, 2) or any(t.dim() != 2 or t.shape != tensors[0].shape or t.dtype != tensors[0].dtype for t in tensors):
+            raise ValueError("one or two [M, N] tensors of the same size and type")
+        first = tensors[0]
+        code = TN_DTYPE_FP8 if scales is not None else _DTYPE.get(first.dtype)
+        if code is None or (scales is not None and first.dtype != _CODES) or not all(t.is_cuda and t.is_contiguous() for t in tensors):
+            raise ValueError("tensors must be contiguous CUDA tensors of float32 or bfloat16, or of float8_e4m3fn together with their scales")
+        m, n = first.shape
+        desc = _Desc()
+        desc.dtype, desc.n_tensors, desc.out_features, desc.in_features = code, len(tensors), m, n
+        ptrs = (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+        desc.tensors = ptrs
+        if scales is not None:
+            shape = (-(-m // TN_FP8_BLOCK), -(-n // TN_FP8_BLOCK))
+            if len(scales) != len(tensors) or any(not (s.is_cuda and s.is_contiguous() and s.dtype == _SCALES and tuple(s.shape) == shape) for s in scales):
+                raise ValueError(f"scales: one contiguous CUDA {list(shape)} tensor of float8_e8m0fnu for each tensor")
+            scale_ptrs = (ctypes.c_void_p * len(tensors))(*[s.data_ptr() for s in scales])
+            desc.scales = scale_ptrs
+        desc.max_tokens, desc.flags, desc.stream = int(max_tokens), TN_FLAG_TRANSPOSE if transpose else 0, _stream()
+        h = ctypes.c_void_p(0)
+        _check(_library().tn_fp8_linear_create(ctypes.byref(h), ctypes.byref(desc)), "tn_fp8_linear_create")
+        self._handle = int(h.value)
+        self.shape, self.n_tensors, self.transpose = (m, n), len(tensors), bool(transpose)
+        self._device = first.device
+        self.M, self.N = self.query(TN_QUERY_OUT_FEATURES), self.query(TN_QUERY_IN_FEATURES)
+        self._segments = len(tensors) if transpose else 1
+
+    def _input(self, x) -> Fp8Rows:
+        if self._handle is None:
+            raise RuntimeError("layer was closed")
+        if not isinstance(x, Fp8Rows):
+            if x.dim() != 2 or x.shape[1] != self.N:
+                raise ValueError(f"x must be [tokens, {self.N}]")
+            x = quantize_fp8(x, self._segments)
+        return x._ready("x", x.rows, self.N // self._segments, self._segments)
+
+    def forward(self, x, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """bf16 [tokens, M] for x in 8 bits (Fp8Rows), or a float32 / bfloat16 tensor, which is quantised first; two
+        tensors' outputs lie beside each other."""
+        x = self._input(x)
+        if out is None:
+            out = torch.empty((x.rows, self.M), dtype=torch.bfloat16, device=self._device)
+        stride = _matrix("out", out, x.rows, self.M, torch.bfloat16)
+        _check(_lib.tn_fp8_linear_forward(self._handle, x.codes.data_ptr(), x.scales.data_ptr(), out.data_ptr(), stride, x.rows, _stream()),
+               "tn_fp8_linear_forward")
+        return out
+
+    __call__ = forward
+
+    def gated(self, x, out: Optional[Fp8Rows] = None) -> Fp8Rows:
+        """silu(x Wg^T) * (x Wu^T) in 8 bits, for a layer of two tensors (Wg, Wu)."""
+        if self.n_tensors != 2 or self.transpose:
+            raise ValueError("gated needs a layer of two tensors that is not transposed")
+        x = self._input(x)
+        m = self.shape[0]
+        out = Fp8Rows.empty(x.rows, m, 1, self._device) if out is None else out._ready("out", x.rows, m, 1)
+        _check(_lib.tn_fp8_linear_gated(self._handle, x.codes.data_ptr(), x.scales.data_ptr(), out.codes.data_ptr(), out.scales.data_ptr(),
+                                        x.rows, _stream()), "tn_fp8_linear_gated")
+        return out
+
+    def quantized_tensor(self, slot: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(codes [M, N], scales [ceil(M / 128), ceil(N / 128)]) of tensor `slot`."""
+        if self._handle is None:
+            raise RuntimeError("layer was closed")
+        m, n = self.shape
+        codes = torch.empty((m, n), dtype=_CODES, device=self._device)
+        scales = torch.empty((-(-m // TN_FP8_BLOCK), -(-n // TN_FP8_BLOCK)), dtype=_SCALES, device=self._device)
+        _check(_lib.tn_fp8_linear_tensor(self._handle, int(slot), codes.data_ptr(), scales.data_ptr(), _stream()), "tn_fp8_linear_tensor")
+        return codes, scales
+
+    def query(self, what: int) -> int:
+        if self._handle is None:
+            raise RuntimeError("layer was closed")
+        value = ctypes.c_int64(0)
+        _check(_library().tn_fp8_linear_query(self._handle, int(what), ctypes.byref(value)), "tn_fp8_linear_query")
+        return int(value.value)
+
+    def close(self) -> None:
+        if self._handle is not None:
+            handle, self._handle = self._handle, None
+            _check(_library().tn_fp8_linear_destroy(handle), "tn_fp8_linear_destroy")
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
