@@ -37,7 +37,7 @@ extern "C" {
 
 #define TN_FP8_BLOCK      128
 #define TN_FP8_MAX_NORM_COLS 16384      /* widest row of tn_rms_norm and its gradients */
-#define TN_FP8_MAX_FEATURES (1 << 22)   /* of tn_fp8_linear, per tensor and side */
+#define TN_FP8_MAX_FEATURES (1 << 21)   /* of tn_fp8_linear, per tensor and side */
 
 /* tn_fp8_linear_desc.dtype, beside TN_DTYPE_F32 and TN_DTYPE_BF16: tensors that are quantised already */
 #define TN_DTYPE_FP8 2

@@ -3,6 +3,7 @@
 
 #include <cstdint>
 #include <new>
+#include <utility>
 
 #include "../../include/tn_fp8.h"
 
@@ -13,6 +14,7 @@ namespace {
 #include "kernels/fp8_rows.hpp"
 #include "kernels/fp8_weight.hpp"
 #include "kernels/fp8_stream.hpp"
+#include "kernels/fp8_gemm.hpp"
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 constexpr int64_t kMaxCols = int64_t(1) << 24;
@@ -149,6 +151,36 @@ int run_stream_gated(const LinearArgs& a, hipStream_t stream) {
     const dim3 grid(unsigned(a.f_pieces / 8), unsigned(div_up(a.tokens, 16 * NT)));
     stream_gated_kernel<NT><<<grid, dim3(1024), 0, stream>>>(a);
     return launched();
+}
+
+template <int TM, int TN, int FORM>
+int run_gemm(GemmArgs g, hipStream_t stream) {
+    using S = GemmShape<TM, TN>;
+    const int64_t n_row = div_up(g.l.tokens, S::BM), n_col = FORM == GEMM_GATED ? g.l.f_pieces / 8 : div_up(int64_t(g.l.f_pieces) * g.l.tensors, 2 * TN);
+    const int64_t items = n_row * n_col * g.n_split;
+    if (items > INT32_MAX / 8) return TN_ERR_UNSUPPORTED;
+    g.n_row = int(n_row);
+    g.n_col = int(n_col);
+    gemm_kernel<TM, TN, FORM><<<dim3(unsigned(div_up(items, 8) * 8)), dim3(256), S::SMEM, stream>>>(g);
+    return launched();
+}
+template <int TM, int TN, int FORM>
+bool allow_gemm() {          // more LDS than a launch gets by default
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_kernel<TM, TN, FORM>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               GemmShape<TM, TN>::SMEM) == hipSuccess;
+}
+template <int FORM>
+bool allow_gemms() {
+    return allow_gemm<8, 8, FORM>() && allow_gemm<4, 8, FORM>();
+}
+template <int FORM>
+int dispatch_gemm(const LinearArgs& a, hipStream_t stream) {
+    GemmArgs g{};
+    g.l = a;
+    g.n_split = 1;
+    g.ktiles_per_split = int(div_up(a.k_blocks, 4) * 4);
+    if (a.tokens > 128) return run_gemm<8, 8, FORM>(g, stream);
+    return run_gemm<4, 8, FORM>(g, stream);
 }
 
 }  // namespace
@@ -329,9 +361,9 @@ int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
     h->packed_bytes = int64_t(h->out_segments) * h->f_blocks * 8 * h->k_blocks * 2048;
     h->scale_bytes = int64_t(h->out_segments) * h->f_blocks * h->scale_stride;
     const hipStream_t st = static_cast<hipStream_t>(d->stream);
-    int rc = TN_OK;
-    if (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
-        hipMalloc(reinterpret_cast<void**>(&h->scales), size_t(h->scale_bytes)) != hipSuccess) {
+    int rc = allow_gemms<GEMM_PLAIN>() && allow_gemms<GEMM_GATED>() ? TN_OK : TN_ERR_HIP;
+    if (rc == TN_OK && (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
+        hipMalloc(reinterpret_cast<void**>(&h->scales), size_t(h->scale_bytes)) != hipSuccess)) {
         (void)hipGetLastError();
         rc = TN_ERR_ALLOC;
     }
@@ -363,8 +395,7 @@ int tn_fp8_linear_forward(tn_fp8_linear_t h, const void* codes, const void* scal
     a.y = y;
     a.y_stride = y_stride;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (div_up(tokens, 64) > 65535) return TN_ERR_UNSUPPORTED;
-    return tokens <= 16 ? run_stream<1>(a, st) : run_stream<4>(a, st);
+    return tokens <= 16 ? run_stream<1>(a, st) : tokens <= 64 ? run_stream<4>(a, st) : dispatch_gemm<GEMM_PLAIN>(a, st);
 }
 
 int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales, void* out_codes, void* out_scales, int64_t tokens, void* stream) {
@@ -380,8 +411,7 @@ int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales
     a.out_scale_stride = o.scale_stride;
     a.spare = o.spare;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (div_up(tokens, 32) > 65535) return TN_ERR_UNSUPPORTED;
-    return tokens <= 16 ? run_stream_gated<1>(a, st) : run_stream_gated<2>(a, st);
+    return tokens <= 16 ? run_stream_gated<1>(a, st) : tokens <= 32 ? run_stream_gated<2>(a, st) : dispatch_gemm<GEMM_GATED>(a, st);
 }
 
 int tn_fp8_linear_tensor(tn_fp8_linear_t h, int32_t slot, void* codes, void* scales, void* stream) {
