@@ -89,8 +89,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     constexpr int W_STEP = FORM == GEMM_GATED ? TH : TN;
     const int first0 = col_tile * (FORM == GEMM_GATED ? TN : 2 * TN), first1 = first0 + (FORM == GEMM_GATED ? a.f_pieces : TH);
     auto weight_rsrc = [&](int first) {
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.packed + int64_t(first) * piece_bytes), 0,
-                                                 max(0, min(all_pieces - first, W_STEP + TH)) * piece_bytes, RSRC);
+        // (a clamp is a vector instruction, and a descriptor from vector registers makes every load a loop)
+        const int there = __builtin_amdgcn_readfirstlane(max(0, min(all_pieces - first, W_STEP + TH)));
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.packed + int64_t(first) * piece_bytes), 0, there * piece_bytes, RSRC);
     };
     const __amdgpu_buffer_rsrc_t rb0 = weight_rsrc(first0), rb1 = weight_rsrc(first1);
     const int fb0 = first0 >> 3, fb1 = FORM == GEMM_GATED ? first1 >> 3 : fb0 + 1;               // the tile's blocks of features
@@ -125,9 +126,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         }
     };
 
-    // fragments: lane l has row (token, or feature) l % 16 and k = 32 * (l / 16) .. + 31
+    // fragments: lane l has row (token, or feature) l % 16, its 16-byte chunks l / 16 and 4 + l / 16
     const int r = lane & 15, kq = lane >> 4;
-    const int oa0 = (wm * TM * 16 + r) * kBlock + (((2 * kq) ^ (r >> 1)) * 16), oa1 = (wm * TM * 16 + r) * kBlock + (((2 * kq + 1) ^ (r >> 1)) * 16);
+    const int oa0 = (wm * TM * 16 + r) * kBlock + ((kq ^ (r >> 1)) * 16), oa1 = (wm * TM * 16 + r) * kBlock + (((4 + kq) ^ (r >> 1)) * 16);
     const int ob = S::A_BYTES + wn * TN * 2048 + lane * 16;
     intx4 fa[TM][2], fb[TN][2];
     floatx4 acc[TM][TN];

@@ -4,13 +4,14 @@
 
 // ---------------------------------------------------------------------------------------------
 // The products multiply an operand W [features][k] (the tensor, or its transpose) held in pieces of 16 features x 128 k, 2 KB,
-// [features / 16][k / 128]: byte (f, k) of a piece at 1024 * ((k / 16) & 1) + 16 * (f + 16 * (k / 32)) + k % 16. Lane l of a
-// wave that reads 16 bytes at 16 * l and at 1024 + 16 * l thus has feature l % 16 and k = 32 * (l / 16) .. + 31, in two contiguous
-// 1 KB loads. Scale bytes lie [features / 128][k / 128], a row padded to a multiple of 4. Features are padded to whole blocks
-// per tensor (zero codes), and so is k, as the rows of activations are.
+// [features / 16][k / 128]: byte (f, k) of a piece at 1024 * (k / 64) + 16 * (f + 16 * (k / 16 % 4)) + k % 16. Lane l of a wave that reads
+// 16 bytes at 16 * l and at 1024 + 16 * l thus has feature l % 16 and the chunks l / 16 and 4 + l / 16 of 16 k each, in two contiguous 1 KB
+// loads. (The order of k in the instruction's operands is free as long as both have the same: all 128 share a scale. This one lets the
+// rows of tokens be read from LDS without conflicts.) Scale bytes lie [features / 128][k / 128], a row padded to a multiple of 4. Features
+// are padded to whole blocks per tensor (zero codes), and so is k, as the rows of activations are.
 // ---------------------------------------------------------------------------------------------
 __host__ __device__ __forceinline__ int piece_offset(int f, int k) {
-    return 1024 * ((k >> 4) & 1) + 16 * (f + 16 * (k >> 5)) + (k & 15);
+    return 1024 * (k >> 6) + 16 * (f + 16 * ((k >> 4) & 3)) + (k & 15);
 }
 
 struct WeightArgs {
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(256) weight_pack_kernel(WeightArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int v = tid + 256 * i, piece = v >> 7, in = v & 127, l = in & 63;
-        const int f = piece * 16 + (l & 15), k = 32 * (l >> 4) + 16 * (in >> 6);
+        const int f = piece * 16 + (l & 15), k = 16 * (l >> 4) + 64 * (in >> 6);
         *reinterpret_cast<uint4*>(a.packed + ((int64_t(fb) * 8 + piece) * a.k_blocks + kb) * 2048 + in * 16) = *reinterpret_cast<const uint4*>(&block[f][k]);
     }
 }
