@@ -78,7 +78,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     const int kt0 = split * g.ktiles_per_split, nk = min(a.k_blocks, kt0 + g.ktiles_per_split) - kt0;
 
     // tokens past the end, and pieces past theirs, are out of the buffers' bounds by the lane's own offset: no memory is read
-    constexpr int RSRC = 0x00020000, OUT = int(0x80000000u);
+    constexpr int RSRC = 0x00020000;
     const int rows = int(min(a.tokens - row0, int64_t(S::BM)));
     const int code_stride = int(a.code_stride), scale_stride = int(a.scale_stride);
     const int piece_bytes = a.k_blocks * 2048;
@@ -103,26 +103,26 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     const int va = (pair * TM * 16 + part * 8 + (lane >> 3)) * code_stride + (((lane & 7) ^ (part * 4 + (lane >> 4))) * 16);
     const int vb = pair * W_STEP * piece_bytes + part * 1024 + lane * 16;
     const int lds_a = (pair * TM * 16 + part * 8) * kBlock, lds_b = S::A_BYTES + pair * TN * 2048 + part * 1024;
-    auto past = [&](int kt) -> int { return kt < nk ? 0 : OUT; };               // tiles past the range: no memory is read
-    auto load_a = [&](int i, int kt, int off, unsigned char* s) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_t*)(s + lds_a + i * 2048), 16, (va + i * 16 * code_stride) | off, (kt0 + kt) * kBlock, 0, 0);
+    // (tiles past the range: the last one once more, into a stage that is not read again)
+    auto load_a = [&](int i, int at, unsigned char* s) {                        // at: K tile in memory
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_t*)(s + lds_a + i * 2048), 16, va + i * 16 * code_stride, at * kBlock, 0, 0);
     };
-    auto load_b = [&](int j, int kt, int off, unsigned char* s) {               // j: fragment 0 .. TN - 1
+    auto load_b = [&](int j, int at, unsigned char* s) {                        // j: fragment 0 .. TN - 1
         __builtin_amdgcn_raw_ptr_buffer_load_lds(j < TH ? rb0 : rb1, (lds_t*)(s + lds_b + j * 2048), 16,
-                                                 (vb + (j < TH ? j : j - TH) * piece_bytes) | off, (kt0 + kt) * 2048, 0, 0);
+                                                 vb + (j < TH ? j : j - TH) * piece_bytes, at * 2048, 0, 0);
     };
+    const int last = kt0 + nk - 1;
     // scale words of four tiles: 64 rows to a load, then the two feature blocks (even and odd lanes). Every wave issues as many.
     constexpr int ROW_LOADS = S::SCALE_ROWS / 64, SCALE_LOADS = (ROW_LOADS + 1 + 3) / 4;
     auto load_scales = [&](int group, unsigned char* s) {
-        const int word = (kt0 >> 2) + group;
+        const int word = min((kt0 >> 2) + group, last >> 2);
 #pragma unroll
         for (int q = 0; q < SCALE_LOADS; ++q) {
             const int n = min(wave + 4 * q, ROW_LOADS);
-            const int off = past(group * 4);
             if (n < ROW_LOADS)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(s + n * 256), 4, ((n * 64 + lane) * scale_stride) | off, word * 4, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(s + n * 256), 4, (n * 64 + lane) * scale_stride, word * 4, 0, 0);
             else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_t*)(s + n * 256), 4, ((lane & 1 ? fb1 : fb0) * a.w_scale_stride) | off, word * 4, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_t*)(s + n * 256), 4, (lane & 1 ? fb1 : fb0) * a.w_scale_stride, word * 4, 0, 0);
         }
     };
 
@@ -158,13 +158,13 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     for (int q = 0; q < 2; ++q) {
         unsigned char* s = smem + q * S::STAGE;
 #pragma unroll
-        for (int i = 0; i < LO; ++i) load_a(i, q, past(q), s);
+        for (int i = 0; i < LO; ++i) load_a(i, min(kt0 + q, last), s);
 #pragma unroll
-        for (int j = 0; j < TH; ++j) load_b(q ? TH + j : j, q, past(q), s);
+        for (int j = 0; j < TH; ++j) load_b(q ? TH + j : j, min(kt0 + q, last), s);
 #pragma unroll
-        for (int i = LO; i < TM; ++i) load_a(i, q, past(q), s);
+        for (int i = LO; i < TM; ++i) load_a(i, min(kt0 + q, last), s);
 #pragma unroll
-        for (int j = 0; j < TH; ++j) load_b(q ? j : TH + j, q, past(q), s);
+        for (int j = 0; j < TH; ++j) load_b(q ? j : TH + j, min(kt0 + q, last), s);
     }
     wait_vmcnt<LA + LB>();                       // the first tile and the scales have landed
     __builtin_amdgcn_s_barrier();
@@ -193,7 +193,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         constexpr int L = HALF ? LB : LA, NA = HALF ? HI : LO;
         constexpr int R0 = HALF ? 2 * LO : TN, R1 = HALF ? TN : 2 * HI;          // reads of the two quadrants
         constexpr int BAR = NM - (NQ >= 8 ? 4 : 1);
-        const int off = past(kt + 2);
+        const int at = min(kt0 + kt + 2, last);
         auto slot = [&](auto slot_c) {
             constexpr int q = decltype(slot_c)::value, quad = q / NQ, m = q % NQ;
             // first half: features outermost (y arrives one by one); second: tokens outermost (hi does)
@@ -233,8 +233,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
 #pragma unroll
             for (int l = 0; l < L; ++l)
                 if (l * BAR / L == q) {
-                    if (l < NA) load_a(I0 + l, kt + 2, off, s);
-                    else load_b((HALF ? Y : X) + l - NA, kt + 2, off, s);
+                    if (l < NA) load_a(I0 + l, at, s);
+                    else load_b((HALF ? Y : X) + l - NA, at, s);
                 }
             if constexpr (HALF == 0 && IDX == 0 && q == 0) load_scales((kt >> 2) + 1, sc_next);
             __builtin_amdgcn_sched_barrier(0);
