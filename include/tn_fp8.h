@@ -100,10 +100,14 @@ typedef struct tn_fp8_linear_s* tn_fp8_linear_t;
  *  out_features, in_features   M and N of each tensor, up to TN_FP8_MAX_FEATURES
  *  tensors      n_tensors device pointers to contiguous [M, N] arrays (the array of pointers is host memory)
  *  scales       TN_DTYPE_FP8 only: device pointers to contiguous [ceil(M / 128), ceil(N / 128)] scale bytes; else ignored
- *  max_tokens   the handle's workspace (partial sums of products whose inputs are split) is sized for calls of up to
- *               this many tokens; larger ones work too, and may take a slower form
+ *  max_tokens   the handle's own workspace (partial sums of products whose inputs are split) is sized for calls of up to
+ *               this many tokens, 64 MB at the most; larger calls work too, and may take a slower form
  *  flags        0 or TN_FLAG_TRANSPOSE: the products take gradients of the outputs and give that of the inputs
  *  stream       on which create enqueues its work; it waits for it before it returns
+ *  workspace, workspace_bytes
+ *               optional device block of the caller, 256-byte aligned, instead of one of the handle's own (NULL, 0): it must outlive the
+ *               handle, and several handles may share it as long as their calls never overlap in time. Any size works; less than
+ *               64 MB may mean a slower form.
  */
 typedef struct tn_fp8_linear_desc {
     int32_t dtype;
@@ -115,6 +119,8 @@ typedef struct tn_fp8_linear_desc {
     int64_t max_tokens;
     int32_t flags;
     void* stream;
+    void* workspace;
+    int64_t workspace_bytes;
 } tn_fp8_linear_desc;
 
 /* On success *out receives the handle, which holds one 8-bit copy of the weights in an order of its own; the caller may

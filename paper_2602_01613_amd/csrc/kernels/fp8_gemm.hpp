@@ -5,25 +5,23 @@
 // ---------------------------------------------------------------------------------------------
 // A workgroup of four waves (2 x 2) computes 32 * TM tokens x 32 * TN features: a wave 16 * TM x 16 * TN in TM x TN accumulators of
 // v_mfma_scale_f32_16x16x128_f8f6f4. A K tile is one block of 128. Both operands go from memory to LDS without passing through
-// registers, two stages of a K tile each; a row of tokens is 128 bytes there, its 16-byte chunk c at position c ^ ((row / 2) % 8), so that
+// registers, two or three stages of a K tile each; a row of tokens is 128 bytes there, its 16-byte chunk c at position c ^ ((row / 2) % 8), so that
 // the 16 rows a read touches at a time fall on 16 different slots of the 64 banks; a piece of the weight is as it is in memory.
 //
 // The wave holds one set of fragments and walks its tile in quadrants of half its tokens (lo, hi) x half its features (x, y):
 //     first half step:   lo * x (reading y),  lo * y (reading hi)
 //     second half step:  hi * y (reading the next tile's lo),  hi * x (reading the next tile's x, into the registers of this one's y)
 // so that each fragment is read one quadrant before its first use into registers whose last use has passed, and x and y change places
-// from tile to tile. What a half step reads ((y, hi), then the next (lo, x)) is free in LDS when it ends: the loads of the tile two further on go
-// there in the half step after it, and have a whole K tile's time to land before the barrier that lets them be read. One barrier a half step.
+// from tile to tile. What a half step reads ((y, hi), then the next (lo, x)) is free in LDS when it ends: the loads of the tile that has this
+// stage next go there in the half step after it, and have a whole K tile's time (with three stages almost two) to land before the barrier that
+// lets them be read. One barrier a half step.
 // Scale bytes: four K tiles of a row in a word, which the instruction picks its byte from; the words of the next four tiles go to LDS
 // while these four are computed.
 // ---------------------------------------------------------------------------------------------
 struct GemmArgs {
     LinearArgs l;
     int32_t n_row, n_col;            // output tiles
-    int32_t n_split;                 // ranges of K
     int32_t ktiles_per_split;        // a multiple of 4; at least one tile in every range
-    float* partial;                  // not null: fp32 sums [split][tokens][ld] of padded features instead of the output
-    int64_t ld;
 };
 
 template <int TM, int TN>
@@ -31,7 +29,11 @@ struct GemmShape {
     static constexpr int BM = 32 * TM, BN = 32 * TN;
     static constexpr int A_BYTES = BM * kBlock, STAGE = (BM + BN) * kBlock;
     static constexpr int SCALE_ROWS = (BM + 63) / 64 * 64, SCALES = (SCALE_ROWS + 64) * 4;       // words of the rows, then of the feature blocks
-    static constexpr int SMEM = 2 * STAGE + 2 * SCALES;
+    // stages: three where LDS holds them (for as many workgroups on a CU), else two
+    static constexpr int LDS = 160 * 1024;
+    static constexpr int PER_CU = 2 * (2 * STAGE + 2 * SCALES) <= LDS ? 2 : 1;
+    static constexpr int NS = PER_CU * (3 * STAGE + 2 * SCALES) <= LDS ? 3 : 2;
+    static constexpr int SMEM = NS * STAGE + 2 * SCALES;
 };
 
 enum GemmForm : int { GEMM_PLAIN = 0, GEMM_GATED = 1 };
@@ -50,7 +52,7 @@ __device__ __forceinline__ void for_constants(F&& f, std::integer_sequence<int, 
 template <int TM, int TN, int FORM>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     using S = GemmShape<TM, TN>;
-    constexpr int LO = (TM + 1) / 2, HI = TM - LO, TH = TN / 2;
+    constexpr int LO = (TM + 1) / 2, HI = TM - LO, TH = TN / 2, NS = S::NS;
     static_assert(TM >= 2 && TN % 2 == 0 && (FORM != GEMM_GATED || TN == 8), "halves of both sides");
     typedef __attribute__((address_space(3))) void lds_t;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -64,11 +66,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     int row_tile, col_tile, split;
     {
         constexpr int BAND = 4;
-        const int n_items = g.n_row * g.n_col * g.n_split, xcd = blockIdx.x & 7;
+        const int n_items = g.n_row * g.n_col * a.n_split, xcd = blockIdx.x & 7;
         const int item = int(int64_t(n_items) * xcd >> 3) + int(blockIdx.x >> 3);
         if (item >= int(int64_t(n_items) * (xcd + 1) >> 3)) return;
-        const int tile = item / g.n_split;
-        split = item - tile * g.n_split;
+        const int tile = item / a.n_split;
+        split = item - tile * a.n_split;
         const int band = tile / (BAND * g.n_col), in_band = tile - band * (BAND * g.n_col);
         const int band_rows = min(BAND, g.n_row - band * BAND);
         col_tile = in_band / band_rows;
@@ -141,7 +143,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         const int which = FORM == GEMM_GATED ? q : (wn * TN) >> 3;
         to[q] = *reinterpret_cast<const unsigned*>(s + S::SCALE_ROWS * 4 + which * 4);
     };
-    unsigned char* const scale_lds = smem + 2 * S::STAGE;
+    unsigned char* const scale_lds = smem + NS * S::STAGE;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -151,22 +153,22 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             asm volatile("" : "+a"(acc[i][j]));
         }
 
-    // prologue: the first group's scales, then both stages in the order in which they are waited for
+    // prologue: the first group's scales, then the stages in the order in which they are waited for
     constexpr int LA = LO + TH, LB = HI + TH;
     load_scales(0, scale_lds);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    for (int q = 0; q < NS; ++q) {
         unsigned char* s = smem + q * S::STAGE;
 #pragma unroll
         for (int i = 0; i < LO; ++i) load_a(i, min(kt0 + q, last), s);
 #pragma unroll
-        for (int j = 0; j < TH; ++j) load_b(q ? TH + j : j, min(kt0 + q, last), s);
+        for (int j = 0; j < TH; ++j) load_b(q & 1 ? TH + j : j, min(kt0 + q, last), s);
 #pragma unroll
         for (int i = LO; i < TM; ++i) load_a(i, min(kt0 + q, last), s);
 #pragma unroll
-        for (int j = 0; j < TH; ++j) load_b(q ? j : TH + j, min(kt0 + q, last), s);
+        for (int j = 0; j < TH; ++j) load_b(q & 1 ? j : TH + j, min(kt0 + q, last), s);
     }
-    wait_vmcnt<LA + LB>();                       // the first tile and the scales have landed
+    wait_vmcnt<(NS - 1) * (LA + LB)>();          // the first tile and the scales have landed
     __builtin_amdgcn_s_barrier();
 #pragma unroll
     for (int i = 0; i < LO; ++i) {
@@ -193,7 +195,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         constexpr int L = HALF ? LB : LA, NA = HALF ? HI : LO;
         constexpr int R0 = HALF ? 2 * LO : TN, R1 = HALF ? TN : 2 * HI;          // reads of the two quadrants
         constexpr int BAR = NM - (NQ >= 8 ? 4 : 1);
-        const int at = min(kt0 + kt + 2, last);
+        const int at = min(kt0 + kt + NS, last);
         auto slot = [&](auto slot_c) {
             constexpr int q = decltype(slot_c)::value, quad = q / NQ, m = q % NQ;
             // first half: features outermost (y arrives one by one); second: tokens outermost (hi does)
@@ -201,7 +203,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             constexpr int j = ((quad == 0) == (HALF == 0) ? X : Y) + jj;
             if constexpr (q == BAR) {
                 __builtin_amdgcn_s_waitcnt(0xC07F);                              // lgkmcnt(0): this wave has read what the half step reads
-                wait_vmcnt<LA + LB>();                                           // its loads for the next half step's reads have landed
+                // its loads for the next half step's reads have landed: with two stages those of half a tile each time, with three, where
+                // x and y have changed places in a stage when it is filled again, those of a whole tile in time for the first half
+                wait_vmcnt<(NS == 2 || HALF) ? (NS - 1) * (LA + LB) : 2 * LA + LB>();
                 __builtin_amdgcn_s_barrier();
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -241,9 +245,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         };
         for_constants(slot, std::make_integer_sequence<int, NM>());
     };
+    int stage = 0;                               // of the current tile, in bytes
     auto tile = [&](auto idx_c, int kt, unsigned char* sc, unsigned char* sc_next) {
         constexpr int IDX = decltype(idx_c)::value;
-        unsigned char *s = smem + (IDX & 1) * S::STAGE, *sn = smem + (1 - (IDX & 1)) * S::STAGE;
+        unsigned char* s = smem + (NS == 2 ? (IDX & 1) * S::STAGE : stage);
+        stage = stage == (NS - 1) * S::STAGE ? 0 : stage + S::STAGE;
+        unsigned char* sn = smem + (NS == 2 ? (1 - (IDX & 1)) * S::STAGE : stage);
         half_step(idx_c, std::integral_constant<int, 0>(), kt, s, sn, sc, sc_next);
         half_step(idx_c, std::integral_constant<int, 1>(), kt, s, sn, sc, sc_next);
     };
@@ -310,11 +317,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         }
     } else {
         const int piece0 = first0 + wn * TN;
-        if (g.partial) {
+        if (a.partial) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
                 const int64_t token = token0 + i * 16;
-                float* p = g.partial + (int64_t(split) * a.tokens + token) * g.ld + piece0 * 16 + kq * 4;
+                float* p = a.partial + (int64_t(split) * a.tokens + token) * a.ld + piece0 * 16 + kq * 4;
                 if (token < a.tokens) {
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
@@ -374,4 +381,41 @@ __global__ void __launch_bounds__(256, 1) gemm_kernel(GemmArgs g) {
 #ifdef __HIP_DEVICE_COMPILE__
     gemm_tile<TM, TN, FORM>(g);
 #endif
+}
+
+// The ranges of K added up in order: a thread takes 4 neighbouring features of a token.
+__global__ void __launch_bounds__(256) gemm_reduce_kernel(LinearArgs a) {
+    const int64_t per_token = a.ld / 4, all = a.tokens * per_token, step = a.tokens * a.ld;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+        const int64_t token = i / per_token;
+        const int f4 = int(i - token * per_token) * 4, tensor = f4 / (a.f_pieces * 16), f = f4 - tensor * a.f_pieces * 16;
+        const float* p = a.partial + token * a.ld + f4;
+        floatx4 v = *reinterpret_cast<const floatx4*>(p);
+        for (int s = 1; s < a.n_split; ++s) v += *reinterpret_cast<const floatx4*>(p + s * step);
+        store4(static_cast<bf16_t*>(a.y) + token * a.y_stride + int64_t(tensor) * a.features + f, a.features - f, v);
+    }
+}
+
+// The same for gate and up, then silu(gate) * up in 8 bits: 16 lanes to a block of 128 features, all of them there.
+__global__ void __launch_bounds__(256) gemm_reduce_gated_kernel(LinearArgs a) {
+    const int64_t per_token = a.ld / 2 / kChunk, all = a.tokens * per_token, step = a.tokens * a.ld;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+        const int64_t token = i / per_token;
+        const int f = int(i - token * per_token) * kChunk;
+        const float* p = a.partial + token * a.ld + f;
+        floatx4 v[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const float* from = p + h * (a.ld / 2) + q * 4;
+                v[h][q] = *reinterpret_cast<const floatx4*>(from);
+                for (int s = 1; s < a.n_split; ++s) v[h][q] += *reinterpret_cast<const floatx4*>(from + s * step);
+            }
+        const floatx4 h0 = gate_value(v[0][0], v[1][0]), h1 = gate_value(v[0][1], v[1][1]);
+        const float h[kChunk] = {h0[0], h0[1], h0[2], h0[3], h1[0], h1[1], h1[2], h1[3]};
+        unsigned char* scales = a.out_scales + token * a.out_scale_stride;
+        quantise_block(h, a.out_codes + token * a.out_code_stride + f, scales + f / kBlock);
+        if (f < 4 * kChunk && f / kChunk < a.spare) scales[(a.f_pieces >> 3) + f / kChunk] = 0;
+    }
 }

@@ -18,6 +18,7 @@ namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 constexpr int64_t kMaxCols = int64_t(1) << 24;
+constexpr int64_t kOwnWorkspace = int64_t(64) << 20;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -99,7 +100,11 @@ struct tn_fp8_linear_s {
     int32_t k_blocks = 0, scale_stride = 0;
     unsigned char *packed = nullptr, *scales = nullptr;
     int64_t packed_bytes = 0, scale_bytes = 0;
+    void* workspace = nullptr;            // partial sums
+    int64_t workspace_bytes = 0;
+    bool own_workspace = false;
     ~tn_fp8_linear_s() {
+        if (own_workspace && workspace) (void)hipFree(workspace);
         if (packed) (void)hipFree(packed);
         if (scales) (void)hipFree(scales);
     }
@@ -137,27 +142,109 @@ LinearArgs linear_args(const tn_fp8_linear_s& h, const void* codes, const void* 
     a.features = h.features;
     a.f_pieces = h.f_blocks * 8;
     a.tensors = h.out_segments;
+    a.n_split = 1;
+    a.ld = int64_t(a.f_pieces) * 16 * a.tensors;
     return a;
 }
 
-template <int NT>
-int run_stream(const LinearArgs& a, hipStream_t stream) {
-    const dim3 grid(unsigned(a.f_pieces * a.tensors), unsigned(div_up(a.tokens, 16 * NT)));
-    stream_kernel<8, 1, NT><<<grid, dim3(512), 0, stream>>>(a);
-    return launched();
+// ---------------------------------------------------------------------------------------------
+// which kernel a product runs on
+// ---------------------------------------------------------------------------------------------
+// Times in us, fitted to measurements on the MI355X (256 CUs) of products of 5120 to 25600 inputs and 1024 to 25600 outputs,
+// 1 to 8192 tokens: within 15 % of most, and the choice by them within 8 % of the best choice at nearly all sizes tried.
+struct TileCost {
+    int tm, tn;
+    double k_tile, rest;      // a workgroup's time for a K tile, and for a tile's beginning and end (with two on a CU: both of them)
+};
+// TN = 8 first: the gated form has only those
+constexpr TileCost kTiles[] = {{2, 8, 0.50, 2.0}, {3, 8, 0.57, 5.0}, {4, 8, 0.72, 7.1}, {5, 8, 0.85, 7.5}, {6, 8, 0.97, 8.0}, {7, 8, 1.10, 8.8}, {8, 8, 1.24, 8.7},
+                               {2, 4, 0.57, 3.1}, {3, 4, 0.69, 3.7}, {4, 4, 0.80, 4.7}, {6, 4, 0.57, 5.0}, {8, 4, 0.71, 6.7}};
+constexpr int kTileCount = int(sizeof(kTiles) / sizeof(kTiles[0])), kGatedTiles = 7;
+constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 10, 16};
+constexpr int kCUs = 256;
+constexpr double kLaunch = 4.0, kReadRate = 5.3e6, kSumsRate = 8e6;      // bytes per us: memory, partial sums
+constexpr double kTilesRate = 25e6, kStreamRate = 14e6, kStreamFarRate = 11e6;       // what is read again, from the caches
+// Memory and computation overlap, but not wholly: of the shorter one this much is added.
+double together(double a, double b) { return a > b ? a + 0.35 * b : b + 0.35 * a; }
+
+struct Choice {
+    int tile = -1;             // index into kTiles; -1: the stream kernel
+    int split = 1, groups = 1;
+    bool fused = false;        // gated: silu(gate) * up by the tile's own workgroup
+    double us = 1e30;
+};
+
+constexpr int tiles_per_cu(const TileCost& t) {
+    const int stage = 32 * (t.tm + t.tn) * kBlock, scales = ((32 * t.tm + 63) / 64 * 64 + 64) * 4;
+    return 2 * (2 * stage + 2 * scales) <= 160 * 1024 ? 2 : 1;
 }
-template <int NT>
-int run_stream_gated(const LinearArgs& a, hipStream_t stream) {
-    const dim3 grid(unsigned(a.f_pieces / 8), unsigned(div_up(a.tokens, 16 * NT)));
-    stream_gated_kernel<NT><<<grid, dim3(1024), 0, stream>>>(a);
+
+Choice choose(const LinearArgs& a, bool gated, int64_t workspace_bytes) {
+    const int64_t pieces = int64_t(a.f_pieces) * a.tensors, weight = pieces * a.k_blocks * 2048;
+    const double outputs = double(a.tokens) * a.ld * 4;       // of one range's partial sums
+    const auto sums = [&](int ranges) { return 3.0 + 2 * ranges * outputs / kSumsRate; };
+    Choice best;
+    // streamed, 16 tokens at a time: the weight comes from memory once, for every further 16 tokens from the caches, and each workgroup
+    // reads its tokens. Pieces to a workgroup: one where there are few; two where one each would leave some CUs two workgroups and
+    // others one (320 pieces of 25600 k, one token: 25.4 us with two to a workgroup, 30 with one); with more than four tokens as many as leave two
+    // workgroups or more to a CU (1600 pieces of 5120 k, 16 tokens: 28 us with four, 33 with one).
+    if (a.tokens <= 16 * 65535 && (!gated || outputs <= double(workspace_bytes))) {
+        Choice c;
+        c.groups = pieces <= kCUs ? 1 : pieces < 2 * kCUs ? 2 : a.tokens <= 4 ? 1 : pieces < 4 * kCUs ? 2 : 4;
+        const double passes = double(div_up(a.tokens, 16));
+        const double cached = (passes * weight + double(pieces) / c.groups * a.tokens * a.k_blocks * kBlock) / (weight < (16 << 20) ? kStreamRate : kStreamFarRate);
+        const double memory = weight / kReadRate;
+        c.us = kLaunch + together(memory, cached) + (gated ? sums(1) : 0);
+        best = c;
+    }
+    for (int t = 0; t < kTileCount; ++t) {
+        const TileCost& cost = kTiles[t];
+        const int per_cu = tiles_per_cu(cost);
+        const int64_t n_row = div_up(a.tokens, 32 * cost.tm), n_col = div_up(pieces, 2 * cost.tn);
+        for (const int split : kSplits) {
+            const bool fused = gated && split == 1 && t < kGatedTiles;
+            const int64_t items = n_row * (fused ? a.f_pieces / 8 : n_col) * split;
+            if (split > 1 && (split * 4 > a.k_blocks || items > 4 * kCUs)) break;
+            if ((split > 1 || (gated && !fused)) && split * outputs > double(workspace_bytes)) break;
+            const int64_t nk = div_up(div_up(a.k_blocks, split), 4) * 4, rounds = div_up(items, int64_t(kCUs) * per_cu);
+            // two workgroups share a CU only where there are enough of them
+            const double alone = per_cu == 2 && items <= kCUs ? 0.6 : 1.0;
+            const double compute = rounds * alone * (double(nk < a.k_blocks ? nk : a.k_blocks) * cost.k_tile + cost.rest);
+            // the weight comes from memory for the first row of tiles; what is read again (and the tokens) from the caches
+            const double memory = weight / kReadRate + double(n_row - 1) * weight / kTilesRate + (split > 1 ? 0 : outputs / 2) / kSumsRate;
+            const double us = kLaunch + together(compute, memory) + (split > 1 || (gated && !fused) ? sums(split) : 0);
+            if (us < best.us) {
+                best.us = us;
+                best.tile = t;
+                best.split = split;
+                best.fused = fused;
+            }
+        }
+    }
+    return best;
+}
+
+// Waves of a workgroup of the stream kernel: as many words of scales (four blocks of k) to each, and at most `most` waves.
+int stream_waves(int k_blocks, int most) {
+    const int words = int(div_up(k_blocks, 4)), rounds = int(div_up(words, most));
+    return int(div_up(words, rounds));
+}
+template <int GROUPS>
+int run_stream(const LinearArgs& a, hipStream_t stream) {
+    const dim3 grid(unsigned(a.f_pieces * a.tensors / GROUPS), unsigned(div_up(a.tokens, 16)));
+    stream_kernel<GROUPS><<<grid, dim3(64 * stream_waves(a.k_blocks, 16)), 0, stream>>>(a);
     return launched();
 }
 
 template <int TM, int TN, int FORM>
-int run_gemm(GemmArgs g, hipStream_t stream) {
+int run_gemm(const LinearArgs& a, hipStream_t stream) {
     using S = GemmShape<TM, TN>;
-    const int64_t n_row = div_up(g.l.tokens, S::BM), n_col = FORM == GEMM_GATED ? g.l.f_pieces / 8 : div_up(int64_t(g.l.f_pieces) * g.l.tensors, 2 * TN);
-    const int64_t items = n_row * n_col * g.n_split;
+    GemmArgs g{};
+    g.l = a;
+    g.ktiles_per_split = int(div_up(div_up(a.k_blocks, a.n_split), 4) * 4);
+    g.l.n_split = int(div_up(a.k_blocks, g.ktiles_per_split));        // no range without a tile
+    const int64_t n_row = div_up(a.tokens, S::BM), n_col = FORM == GEMM_GATED ? a.f_pieces / 8 : div_up(int64_t(a.f_pieces) * a.tensors, 2 * TN);
+    const int64_t items = n_row * n_col * g.l.n_split;
     if (items > INT32_MAX / 8) return TN_ERR_UNSUPPORTED;
     g.n_row = int(n_row);
     g.n_col = int(n_col);
@@ -169,18 +256,38 @@ bool allow_gemm() {          // more LDS than a launch gets by default
     return hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_kernel<TM, TN, FORM>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                GemmShape<TM, TN>::SMEM) == hipSuccess;
 }
-template <int FORM>
-bool allow_gemms() {
-    return allow_gemm<8, 8, FORM>() && allow_gemm<4, 8, FORM>();
+template <int FORM, int... T>
+bool allow_gemms(std::integer_sequence<int, T...>) {
+    return (allow_gemm<kTiles[T].tm, kTiles[T].tn, FORM>() && ...);
 }
-template <int FORM>
-int dispatch_gemm(const LinearArgs& a, hipStream_t stream) {
-    GemmArgs g{};
-    g.l = a;
-    g.n_split = 1;
-    g.ktiles_per_split = int(div_up(a.k_blocks, 4) * 4);
-    if (a.tokens > 128) return run_gemm<8, 8, FORM>(g, stream);
-    return run_gemm<4, 8, FORM>(g, stream);
+template <int FORM, int... T>
+int run_tile(const LinearArgs& a, int tile, hipStream_t stream, std::integer_sequence<int, T...>) {
+    int rc = TN_ERR_UNSUPPORTED;
+    (void)((T == tile ? (rc = run_gemm<kTiles[T].tm, kTiles[T].tn, FORM>(a, stream), true) : false) || ...);
+    return rc;
+}
+
+int run_product(const tn_fp8_linear_s& h, LinearArgs a, bool gated, hipStream_t stream) {
+    const Choice c = choose(a, gated, h.workspace_bytes);
+    const bool in_parts = c.split > 1 || (gated && !c.fused);
+    if (in_parts) a.partial = static_cast<float*>(h.workspace);
+    a.n_split = c.split;
+    int rc;
+    if (c.tile < 0) {
+        rc = c.groups == 1 ? run_stream<1>(a, stream) : c.groups == 2 ? run_stream<2>(a, stream) : run_stream<4>(a, stream);
+    } else if (c.fused) {
+        rc = run_tile<GEMM_GATED>(a, c.tile, stream, std::make_integer_sequence<int, kGatedTiles>());
+    } else {
+        rc = run_tile<GEMM_PLAIN>(a, c.tile, stream, std::make_integer_sequence<int, kTileCount>());
+    }
+    if (rc != TN_OK || !in_parts) return rc;
+    const int64_t ktiles = div_up(div_up(a.k_blocks, a.n_split), 4) * 4;
+    a.n_split = int(div_up(a.k_blocks, ktiles));              // as the tiles took it
+    const int64_t groups = div_up(a.tokens * a.ld / (gated ? 2 * kChunk : 4), 256);
+    const dim3 grid(unsigned(groups < 8 * kCUs ? groups : 8 * kCUs));
+    if (gated) gemm_reduce_gated_kernel<<<grid, dim3(256), 0, stream>>>(a);
+    else gemm_reduce_kernel<<<grid, dim3(256), 0, stream>>>(a);
+    return launched();
 }
 
 }  // namespace
@@ -339,6 +446,7 @@ int tn_silu_gate_gradients(int32_t dtype, int64_t rows, int64_t cols, const void
 
 int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
     if (!out || !d || !d->tensors || d->out_features < 1 || d->in_features < 1 || d->max_tokens < 1) return TN_ERR_INVALID_ARG;
+    if (d->workspace ? d->workspace_bytes < 1 || !aligned(d->workspace, 256) : d->workspace_bytes != 0) return TN_ERR_INVALID_ARG;
     const bool given = d->dtype == TN_DTYPE_FP8;
     if ((!given && !float_type(d->dtype)) || (given && !d->scales) || d->n_tensors < 1 || d->n_tensors > 2 || (d->flags & ~TN_FLAG_TRANSPOSE))
         return TN_ERR_INVALID_ARG;
@@ -361,11 +469,25 @@ int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
     h->packed_bytes = int64_t(h->out_segments) * h->f_blocks * 8 * h->k_blocks * 2048;
     h->scale_bytes = int64_t(h->out_segments) * h->f_blocks * h->scale_stride;
     const hipStream_t st = static_cast<hipStream_t>(d->stream);
-    int rc = allow_gemms<GEMM_PLAIN>() && allow_gemms<GEMM_GATED>() ? TN_OK : TN_ERR_HIP;
+    int rc = allow_gemms<GEMM_PLAIN>(std::make_integer_sequence<int, kTileCount>()) && allow_gemms<GEMM_GATED>(std::make_integer_sequence<int, kGatedTiles>()) ? TN_OK : TN_ERR_HIP;
     if (rc == TN_OK && (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
         hipMalloc(reinterpret_cast<void**>(&h->scales), size_t(h->scale_bytes)) != hipSuccess)) {
         (void)hipGetLastError();
         rc = TN_ERR_ALLOC;
+    }
+    if (d->workspace) {
+        h->workspace = d->workspace;
+        h->workspace_bytes = d->workspace_bytes;
+    } else if (rc == TN_OK) {
+        // the most ranges of K there are, at max_tokens: more than the products ask for, and no more than 64 MB
+        const int64_t want = div_up(16 * d->max_tokens * h->out_segments * h->f_blocks * kBlock * 4, 256) * 256;
+        h->workspace_bytes = want < kOwnWorkspace ? want : kOwnWorkspace;
+        h->own_workspace = true;
+        if (hipMalloc(&h->workspace, size_t(h->workspace_bytes)) != hipSuccess) {
+            (void)hipGetLastError();
+            h->workspace = nullptr;
+            rc = TN_ERR_ALLOC;
+        }
     }
     for (int i = 0; rc == TN_OK && i < h->tensors; ++i) {
         WeightArgs a = weight_args(*h, i);
@@ -394,8 +516,7 @@ int tn_fp8_linear_forward(tn_fp8_linear_t h, const void* codes, const void* scal
     LinearArgs a = linear_args(*h, codes, scales, tokens);
     a.y = y;
     a.y_stride = y_stride;
-    const hipStream_t st = static_cast<hipStream_t>(stream);
-    return tokens <= 16 ? run_stream<1>(a, st) : tokens <= 64 ? run_stream<4>(a, st) : dispatch_gemm<GEMM_PLAIN>(a, st);
+    return run_product(*h, a, false, static_cast<hipStream_t>(stream));
 }
 
 int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales, void* out_codes, void* out_scales, int64_t tokens, void* stream) {
@@ -410,8 +531,7 @@ int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales
     a.out_code_stride = o.code_stride;
     a.out_scale_stride = o.scale_stride;
     a.spare = o.spare;
-    const hipStream_t st = static_cast<hipStream_t>(stream);
-    return tokens <= 16 ? run_stream_gated<1>(a, st) : tokens <= 32 ? run_stream_gated<2>(a, st) : dispatch_gemm<GEMM_GATED>(a, st);
+    return run_product(*h, a, true, static_cast<hipStream_t>(stream));
 }
 
 int tn_fp8_linear_tensor(tn_fp8_linear_t h, int32_t slot, void* codes, void* scales, void* stream) {
@@ -430,7 +550,7 @@ int tn_fp8_linear_query(tn_fp8_linear_t h, int32_t what, int64_t* value) {
         case TN_QUERY_IN_FEATURES: *value = int64_t(h->k_segments) * h->k_cols; return TN_OK;
         case TN_QUERY_PARAM_COUNT: *value = h->tensors * h->m * h->n; return TN_OK;
         case TN_QUERY_PACKED_BYTES: *value = h->packed_bytes + h->scale_bytes; return TN_OK;
-        case TN_QUERY_WORKSPACE_BYTES: *value = 0; return TN_OK;
+        case TN_QUERY_WORKSPACE_BYTES: *value = h->workspace_bytes; return TN_OK;
         default: return TN_ERR_INVALID_ARG;
     }
 }

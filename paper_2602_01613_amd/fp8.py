@@ -52,6 +52,8 @@ class _Desc(ctypes.Structure):
         ("max_tokens", ctypes.c_int64),
         ("flags", ctypes.c_int32),
         ("stream", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
     ]
 
 
@@ -279,11 +281,12 @@ class Fp8Linear:
 
     tensors  one or two contiguous CUDA tensors of float32 or bfloat16, quantised in blocks of 128 x 128; or, with `scales`,
              float8_e4m3fn codes and their float8_e8m0fnu scales [ceil(M / 128), ceil(N / 128)]
+    workspace  a block of CUDA memory that several layers may share (up to 64 MB are of use), instead of one of the layer's own
     transpose=True  the layer maps gradients of the outputs (two segments for two tensors) to that of the inputs
     """
 
     def __init__(self, tensors: Sequence[torch.Tensor], max_tokens: int, transpose: bool = False,
-                 scales: Optional[Sequence[torch.Tensor]] = None):
+                 scales: Optional[Sequence[torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None):
         self._handle = None
         if not torch.cuda.is_available():
             raise RuntimeError("Fp8Linear needs a GPU: there is no CPU path")
@@ -305,6 +308,11 @@ class Fp8Linear:
                 raise ValueError(f"scales: one contiguous CUDA {list(shape)} tensor of float8_e8m0fnu for each tensor")
             scale_ptrs = (ctypes.c_void_p * len(tensors))(*[s.data_ptr() for s in scales])
             desc.scales = scale_ptrs
+        self._workspace = workspace          # keep the caller's block alive as long as the handle
+        if workspace is not None:
+            if not (workspace.is_cuda and workspace.is_contiguous() and workspace.numel() > 0):
+                raise ValueError("workspace must be a contiguous CUDA tensor")
+            desc.workspace, desc.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         desc.max_tokens, desc.flags, desc.stream = int(max_tokens), TN_FLAG_TRANSPOSE if transpose else 0, _stream()
         h = ctypes.c_void_p(0)
         _check(_library().tn_fp8_linear_create(ctypes.byref(h), ctypes.byref(desc)), "tn_fp8_linear_create")

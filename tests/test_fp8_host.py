@@ -162,6 +162,7 @@ def _desc(**change):
     (dict(out_features=0), INVALID), (dict(in_features=-4), INVALID), (dict(max_tokens=0), INVALID), (dict(flags=2), INVALID),
     (dict(tensors=None), INVALID), (dict(tensors=[None]), INVALID), (dict(tensors=[A + 1]), INVALID), (dict(dtype=2), INVALID),
     (dict(dtype=2, scales=[None]), INVALID), (dict(n_tensors=2, tensors=[A, None]), INVALID),
+    (dict(workspace=A + 16, workspace_bytes=1024), INVALID), (dict(workspace=A, workspace_bytes=0), INVALID), (dict(workspace_bytes=1024), INVALID),
     (dict(out_features=1 << 23), UNSUPPORTED), (dict(in_features=1 << 40), UNSUPPORTED), (dict(max_tokens=1 << 40), UNSUPPORTED)])
 def test_layer_descriptions_refused(change, status):
     h = ctypes.c_void_p(0)

@@ -174,6 +174,25 @@ def test_more_tokens_than_the_handle_was_made_for():
     check_product(tn.Fp8Linear([dev(w[0])], 1)(dev(x)), eight(rounded(x)), eight(w[0], 128))
 
 
+def test_ranges_of_inputs_in_a_shared_workspace():
+    """Sizes whose inputs are split (partial sums in the workspace): a block that two layers share, blocks too small for it, and the layer's own."""
+    rng = np.random.default_rng(14)
+    m, n, tokens = 300, 4000, 70
+    w, x = weights_of(rng, m, n, 2), rounded(rng.standard_normal((tokens, n)))
+    x8, w8 = eight(x), np.concatenate([eight(v, 128) for v in w])
+    block = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    layers = [tn.Fp8Linear([dev(v) for v in w], tokens, workspace=s) for s in (block, block, block[:256], None)]
+    assert layers[0].query(tn.TN_QUERY_WORKSPACE_BYTES) == 1 << 24 and layers[3].query(tn.TN_QUERY_WORKSPACE_BYTES) > 0
+    gated = []
+    for layer in layers:
+        check_product(layer(dev(x)), x8, w8)
+        gated.append(host(layer.gated(dev(x)).values()))
+    for g in gated[1:]:                       # other orders of the sums: a code here and there is its neighbour
+        assert (g != gated[0]).mean() < 1e-2
+    with pytest.raises(ValueError):
+        tn.Fp8Linear([dev(w[0])], 1, workspace=block.cpu())
+
+
 def test_output_offsets_past_32_bits():
     rng = np.random.default_rng(5)
     tokens, m, n = (1 << 31) // 8200 + 300, 8200, 128
