@@ -28,14 +28,29 @@ __device__ __forceinline__ unsigned scale_byte(unsigned a) {
 // 2^-e for that byte (at most 247): exact, and so is the product with it but for results below fp32's least
 __device__ __forceinline__ float inverse_scale(unsigned byte) { return __uint_as_float((254u - byte) << 23); }
 
-// Four codes in a word. The operands are at most 448 after scaling; what is not finite becomes NaN first, so that no mode bit
-// of the conversion (saturation of infinities) matters.
+// Four codes in a word, of finite values that are at most 448 after scaling
+__device__ __forceinline__ unsigned finite_codes4(float a, float b, float c, float d, float inv) {
+    const unsigned w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0u, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+}
+// The same of any values: what is not finite becomes NaN first, so that no mode bit of the conversion (saturation of infinities)
+// matters.
 __device__ __forceinline__ float nan_unless_finite(float v) {
     return (__float_as_uint(v) & 0x7fffffffu) < 0x7f800000u ? v : __uint_as_float(0x7fc00000u);
 }
 __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, float inv) {
-    unsigned w = __builtin_amdgcn_cvt_pk_fp8_f32(nan_unless_finite(a) * inv, nan_unless_finite(b) * inv, 0u, false);
-    return __builtin_amdgcn_cvt_pk_fp8_f32(nan_unless_finite(c) * inv, nan_unless_finite(d) * inv, w, true);
+    return finite_codes4(nan_unless_finite(a), nan_unless_finite(b), nan_unless_finite(c), nan_unless_finite(d), inv);
+}
+
+// 1 / (1 + exp(-v)) to 4 units of fp32's last place, in 8 instructions where expf and a division take 30: the exponent v * log2(e) in two parts,
+// of which the hardware's 2^x takes the first. Past +-100 the result does not change (0 and 1); a NaN comes out as something finite, and
+// makes a NaN where it is multiplied with v itself.
+__device__ __forceinline__ float sigmoid(float v) {
+    const float c = __builtin_amdgcn_fmed3f(v, -100.f, 100.f);
+    const float t = c * -1.44269504f;
+    const float rest = fmaf(c, -1.44269504f, -t) + c * -1.92596299e-8f;
+    const float e = __builtin_amdgcn_exp2f(t);
+    return __builtin_amdgcn_rcpf(1.f + fmaf(e, rest * 0.693147181f, e));
 }
 
 // Maximum over a row of 16 lanes, left in all of them: rotations by 8, 4, 2 and 1 within the row.
@@ -60,18 +75,42 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// 8 elements at p, of which the first n exist (the others are 0): rows of any alignment the type has
+// 8 elements at p, of which the first n exist (the others are 0), as they are in memory: rows of any alignment the type has.
+// Two bf16 stay in a word (as an array of bf16 the compiler gives each a register of its own).
+template <typename T>
+struct Chunk;
+template <>
+struct Chunk<float> {
+    float v[kChunk];
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+template <>
+struct Chunk<bf16_t> {
+    unsigned w[kChunk / 2];
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+};
+template <typename T>
+__device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
+    Chunk<T> c;
+    if (n >= kChunk) {
+        __builtin_memcpy(&c, p, sizeof(c));
+    } else {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) c.v[i] = i < n ? p[i] : 0.f;
+        } else {
+            const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+            for (int i = 0; i < kChunk; i += 2) c.w[i >> 1] = (i < n ? unsigned(q[i]) : 0u) | (i + 1 < n ? unsigned(q[i + 1]) << 16 : 0u);
+        }
+    }
+    return c;
+}
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float (&v)[kChunk]) {
-    if (n >= kChunk) {
-        T t[kChunk];
-        __builtin_memcpy(t, p, sizeof(t));
+    const Chunk<T> c = load_chunk(p, n);
 #pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = float(t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kChunk; ++i) v[i] = i < n ? float(p[i]) : 0.f;
-    }
+    for (int i = 0; i < kChunk; ++i) v[i] = c[i];
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float (&v)[kChunk]) {
@@ -87,14 +126,28 @@ __device__ __forceinline__ void store8(T* p, int n, const float (&v)[kChunk]) {
     }
 }
 
-// The 16 lanes of a block quantise it: 8 codes go to `codes`, one lane writes the scale byte. All 16 must be here.
+// The 16 lanes of a block quantise it: 8 codes go to `codes`, one lane writes the scale byte. All 16 must be here. The magnitudes
+// are first taken as they are: an infinity or a NaN is larger than any finite one and shows in the maximum.
 __device__ __forceinline__ void quantise_block(const float (&v)[kChunk], unsigned char* codes, unsigned char* scale) {
     unsigned a = 0;
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) a = max(a, finite_magnitude(v[i]));
-    const unsigned byte = scale_byte(row16_max(a));
-    const float inv = inverse_scale(byte);
-    *reinterpret_cast<uint2*>(codes) = make_uint2(codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv));
+    for (int i = 0; i < kChunk; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
+    a = row16_max(a);
+    unsigned byte;
+    uint2 c;
+    if (a < 0x7f800000u) {
+        byte = scale_byte(a);
+        const float inv = inverse_scale(byte);
+        c = make_uint2(finite_codes4(v[0], v[1], v[2], v[3], inv), finite_codes4(v[4], v[5], v[6], v[7], inv));
+    } else {                                             // the same for the 16 lanes
+        a = 0;
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) a = max(a, finite_magnitude(v[i]));
+        byte = scale_byte(row16_max(a));
+        const float inv = inverse_scale(byte);
+        c = make_uint2(codes4(v[0], v[1], v[2], v[3], inv), codes4(v[4], v[5], v[6], v[7], inv));
+    }
+    *reinterpret_cast<uint2*>(codes) = c;
     if ((threadIdx.x & 15) == 0) *scale = static_cast<unsigned char>(byte);
 }
 

@@ -55,14 +55,14 @@ __global__ void __launch_bounds__(256) row_kernel(RowArgs a) {
         if constexpr (OP == ROW_GATE) {
             float h[kChunk];
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) h[i] = gate[i] * (1.f / (1.f + expf(-gate[i]))) * up[i];
+            for (int i = 0; i < kChunk; ++i) h[i] = gate[i] * sigmoid(gate[i]) * up[i];
             put_chunk<T>(a, row, 0, at, h);
         } else {
             float dh[kChunk], dg[kChunk], du[kChunk];
             load8(static_cast<const T*>(a.dh) + row * a.dh_stride + at, n, dh);
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) {
-                const float sig = 1.f / (1.f + expf(-gate[i]));
+                const float sig = sigmoid(gate[i]);
                 dg[i] = dh[i] * up[i] * sig * (1.f + gate[i] * (1.f - sig));
                 du[i] = dh[i] * gate[i] * sig;
             }

@@ -45,38 +45,37 @@ bool float_type(int32_t dtype) { return dtype == TN_DTYPE_F32 || dtype == TN_DTY
 // ---------------------------------------------------------------------------------------------
 // norm
 // ---------------------------------------------------------------------------------------------
-// Waves to a row and chunks to a lane: `chunks` of 8 elements have to fit WAVES * 64 * NC.
-template <typename T, int WAVES, int NC>
-int run_norm(const NormArgs& a, hipStream_t stream) {
-    const int64_t groups = WAVES == 1 ? div_up(a.rows, 4) : a.rows;
-    rms_norm_kernel<T, WAVES, NC><<<dim3(unsigned(groups)), dim3(WAVES == 1 ? 256 : WAVES * 64), 0, stream>>>(a);
+// Threads of a workgroup that shares a row of `chunks` chunks, NC to a thread
+unsigned row_threads(int64_t chunks, int nc) { return unsigned(div_up(chunks, 64 * nc) * 64); }
+
+template <typename T, int NC>
+int run_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
+    rms_norm_kernel<T, NC, false><<<dim3(unsigned(a.rows)), dim3(row_threads(chunks, NC)), 0, stream>>>(a);
     return launched();
 }
 template <typename T>
 int dispatch_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
-    if (chunks <= 64) return run_norm<T, 1, 1>(a, stream);
-    if (chunks <= 256) return run_norm<T, 4, 1>(a, stream);
-    if (chunks <= 512) return run_norm<T, 4, 2>(a, stream);
-    if (chunks <= 768) return run_norm<T, 4, 3>(a, stream);
-    if (chunks <= 1024) return run_norm<T, 4, 4>(a, stream);
-    return run_norm<T, 16, 2>(a, stream);
+    if (chunks <= 64) {
+        rms_norm_kernel<T, 1, true><<<dim3(unsigned(div_up(a.rows, 4))), dim3(256), 0, stream>>>(a);
+        return launched();
+    }
+    // one chunk to a thread as far as a workgroup goes: more waves with their loads under way (8192 rows of 5120: 72 us with 10 waves, 93
+    // with 5 of two chunks each)
+    return chunks <= 1024 ? run_norm<T, 1>(a, chunks, stream) : run_norm<T, 2>(a, chunks, stream);
 }
 
-int64_t norm_grad_groups(int64_t rows) { return rows < 512 ? rows : 512; }
-
-template <typename T, int WAVES, int NC>
-int run_norm_grad(const NormGradArgs& a, int64_t groups, hipStream_t stream) {
-    norm_grad_kernel<T, WAVES, NC><<<dim3(unsigned(groups)), dim3(WAVES * 64), 0, stream>>>(a);
-    return launched();
+// Workgroups of the gradient's one pass: what the 256 CUs hold at a time, and no more, since each adds a row of partial sums. (8192 rows of
+// 5120: 79 us with 256 workgroups of 10 waves, 94 with 409; 4096 rows of 1024: 16 us with 1280 of two waves, 25 with 3840.)
+int64_t norm_grad_groups(int64_t rows, int64_t cols) {
+    const int64_t waves = div_up(div_up(cols, kChunk), 64), groups = 256 * (waves < 10 ? 10 / waves : 1);
+    return rows < groups ? rows : groups;
 }
+
 template <typename T>
 int dispatch_norm_grad(const NormGradArgs& a, int64_t chunks, int64_t groups, hipStream_t stream) {
-    if (chunks <= 64) return run_norm_grad<T, 1, 1>(a, groups, stream);
-    if (chunks <= 256) return run_norm_grad<T, 4, 1>(a, groups, stream);
-    if (chunks <= 512) return run_norm_grad<T, 4, 2>(a, groups, stream);
-    if (chunks <= 768) return run_norm_grad<T, 4, 3>(a, groups, stream);
-    if (chunks <= 1024) return run_norm_grad<T, 4, 4>(a, groups, stream);
-    return run_norm_grad<T, 16, 2>(a, groups, stream);
+    if (chunks <= 1024) norm_grad_kernel<T, 1><<<dim3(unsigned(groups)), dim3(row_threads(chunks, 1)), 0, stream>>>(a);
+    else norm_grad_kernel<T, 2><<<dim3(unsigned(groups)), dim3(row_threads(chunks, 2)), 0, stream>>>(a);
+    return launched();
 }
 
 template <int OP>
@@ -357,7 +356,7 @@ int tn_rms_norm(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_
 int64_t tn_rms_norm_gradients_workspace(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1) return TN_ERR_INVALID_ARG;
     if (rows > kMaxRows || cols > TN_FP8_MAX_NORM_COLS) return TN_ERR_UNSUPPORTED;
-    return norm_grad_groups(rows) * cols * 4;
+    return norm_grad_groups(rows, cols) * cols * 4;
 }
 
 int tn_rms_norm_gradients(int32_t dtype, int64_t rows, int64_t cols, const void* dy, int64_t dy_stride, const void* s,
@@ -368,7 +367,7 @@ int tn_rms_norm_gradients(int32_t dtype, int64_t rows, int64_t cols, const void*
     if (need < 0) return int(need);
     if (!aligned(dweight, 4) || (dweight && need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))) return TN_ERR_INVALID_ARG;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t groups = norm_grad_groups(rows);
+    const int64_t groups = norm_grad_groups(rows, cols);
     if (rows > 0) {
         if (!matrix_ok(dy, dy_stride, cols, dtype) || !matrix_ok(s, s_stride, cols, dtype) || !matrix_ok(dx, dx_stride, cols, dtype) ||
             (dsum && !matrix_ok(dsum, dsum_stride, cols, dtype)) || !aligned(weight, unsigned(element_bytes(dtype))))
@@ -392,7 +391,7 @@ int tn_rms_norm_gradients(int32_t dtype, int64_t rows, int64_t cols, const void*
         if (rc != TN_OK) return rc;
     }
     if (!dweight) return TN_OK;
-    norm_grad_reduce_kernel<<<dim3(unsigned(div_up(cols, 64))), dim3(1024), 0, st>>>(static_cast<const float*>(workspace), int(groups), int(cols), dweight);
+    norm_grad_reduce_kernel<<<dim3(unsigned(div_up(cols, 32))), dim3(1024), 0, st>>>(static_cast<const float*>(workspace), int(groups), int(cols), dweight);
     return launched();
 }
 

@@ -93,16 +93,25 @@ def _check(status: int, where: str) -> None:
         raise TNLinearError(status, where)
 
 
+# The binding's own time is most of a small call's. torch.cuda.current_stream() builds an object (2.8 us); this is what it asks (0.1).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """The current HIP stream of the current device."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch._C._cuda_getDevice())
 
 
 def _matrix(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype) -> int:
     """The row stride of t, a CUDA [rows, cols] matrix of dtype whose rows are contiguous and apart."""
-    if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols):
+    if not (t.dtype is dtype and t.shape == (rows, cols) and t.is_cuda):
         raise ValueError(f"{name} must be a CUDA [{rows}, {cols}] tensor of {dtype}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-    stride = t.stride(0) if rows > 1 else cols
-    if (cols > 1 and t.stride(1) != 1) or stride < cols:
+    stride, step = t.stride()
+    if rows <= 1:
+        stride = cols
+    if (step != 1 and cols > 1) or stride < cols:
         raise ValueError(f"{name}: elements of a row must be contiguous and rows must not overlap (strides {t.stride()})")
     return stride
 
@@ -149,12 +158,15 @@ class Fp8Rows:
         return new
 
     def values(self, segment: int = 0) -> torch.Tensor:
-        start = segment * (-(-self.cols // TN_FP8_BLOCK) * TN_FP8_BLOCK)
-        return self.codes[:, start:start + self.cols]
+        if self.codes.shape[1] == self.cols:
+            return self.codes
+        return self.codes.narrow(1, segment * (-(-self.cols // TN_FP8_BLOCK) * TN_FP8_BLOCK), self.cols)
 
     def block_scales(self, segment: int = 0) -> torch.Tensor:
         blocks = -(-self.cols // TN_FP8_BLOCK)
-        return self.scales[:, segment * blocks:(segment + 1) * blocks]
+        if self.scales.shape[1] == blocks:
+            return self.scales
+        return self.scales.narrow(1, segment * blocks, blocks)
 
     def _ready(self, name: str, rows: int, cols: int, segments: int) -> "Fp8Rows":
         if (self.rows, self.cols, self.segments) != (rows, cols, segments):
