@@ -32,11 +32,12 @@ struct GemmShape {
     // stages: three where LDS holds them (for as many workgroups on a CU), else two
     static constexpr int LDS = 160 * 1024;
     static constexpr int PER_CU = 2 * (2 * STAGE + 2 * SCALES) <= LDS ? 2 : 1;
-    static constexpr int NS = PER_CU * (3 * STAGE + 2 * SCALES) <= LDS ? 3 : 2;
-    static constexpr int SMEM = NS * STAGE + 2 * SCALES;
+    static constexpr int NS = PER_CU * (3 * STAGE + 2 * SCALES + (TN == 8 ? 2 * BM * 4 : 0)) <= LDS ? 3 : 2;
+    static constexpr int SMEM = NS * STAGE + 2 * SCALES + (TN == 8 ? 2 * BM * 4 : 0);            // and the gated form's maxima
 };
 
-enum GemmForm : int { GEMM_PLAIN = 0, GEMM_GATED = 1 };
+// what becomes of the sums: y in bf16, silu(gate) * up in 8 bits, or fp32 to the workspace
+enum GemmForm : int { GEMM_PLAIN = 0, GEMM_GATED = 1, GEMM_PARTIAL = 2 };
 
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
@@ -55,6 +56,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     constexpr int LO = (TM + 1) / 2, HI = TM - LO, TH = TN / 2, NS = S::NS;
     static_assert(TM >= 2 && TN % 2 == 0 && (FORM != GEMM_GATED || TN == 8), "halves of both sides");
     typedef __attribute__((address_space(3))) void lds_t;
+    typedef unsigned int uintx4 __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const LinearArgs& a = g.l;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -62,41 +64,47 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     const int wm = wave >> 1, wn = wave & 1;
 
     // XCD x takes a contiguous eighth of the tiles in bands of four token tiles (tokens fastest), so that the 32 tiles that it runs at
-    // a time share 4 + 8 operand panels in its L2
-    int row_tile, col_tile, split;
-    {
+    // a time share 4 + 8 operand panels in its L2. A launch has no more workgroups than the chip holds: each takes every so many of its
+    // XCD's tiles, and brings the first stages of the next one while it stores this one.
+    const int n_items = g.n_row * g.n_col * a.n_split, xcd = blockIdx.x & 7;
+    const int end_item = int(int64_t(n_items) * (xcd + 1) >> 3), step_item = gridDim.x >> 3;
+    int item = int(int64_t(n_items) * xcd >> 3) + int(blockIdx.x >> 3);
+    if (item >= end_item) return;
+    struct Place {
+        int row_tile, col_tile, split;
+    };
+    auto place_of = [&](int at) {
         constexpr int BAND = 4;
-        const int n_items = g.n_row * g.n_col * a.n_split, xcd = blockIdx.x & 7;
-        const int item = int(int64_t(n_items) * xcd >> 3) + int(blockIdx.x >> 3);
-        if (item >= int(int64_t(n_items) * (xcd + 1) >> 3)) return;
-        const int tile = item / a.n_split;
-        split = item - tile * a.n_split;
+        Place p;
+        const int tile = at / a.n_split;
+        p.split = __builtin_amdgcn_readfirstlane(at - tile * a.n_split);
         const int band = tile / (BAND * g.n_col), in_band = tile - band * (BAND * g.n_col);
         const int band_rows = min(BAND, g.n_row - band * BAND);
-        col_tile = in_band / band_rows;
-        row_tile = band * BAND + in_band - col_tile * band_rows;
-    }
-    const int64_t row0 = int64_t(row_tile) * S::BM;
-    const int kt0 = split * g.ktiles_per_split, nk = min(a.k_blocks, kt0 + g.ktiles_per_split) - kt0;
+        p.col_tile = __builtin_amdgcn_readfirstlane(in_band / band_rows);
+        p.row_tile = __builtin_amdgcn_readfirstlane(band * BAND + in_band - p.col_tile * band_rows);
+        return p;
+    };
 
     // tokens past the end, and pieces past theirs, are out of the buffers' bounds by the lane's own offset: no memory is read
     constexpr int RSRC = 0x00020000;
-    const int rows = int(min(a.tokens - row0, int64_t(S::BM)));
     const int code_stride = int(a.code_stride), scale_stride = int(a.scale_stride);
     const int piece_bytes = a.k_blocks * 2048;
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.codes + row0 * a.code_stride), 0, rows * code_stride, RSRC);
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.scales + row0 * a.scale_stride), 0, rows * scale_stride, RSRC);
     const int all_pieces = a.f_pieces * a.tensors;
-    // pieces of the two feature halves: wave column w, fragment j of half 0 or 1 is piece first[half] + w * W_STEP + j
-    constexpr int W_STEP = FORM == GEMM_GATED ? TH : TN;
-    const int first0 = col_tile * (FORM == GEMM_GATED ? TN : 2 * TN), first1 = first0 + (FORM == GEMM_GATED ? a.f_pieces : TH);
-    auto weight_rsrc = [&](int first) {
-        // (a clamp is a vector instruction, and a descriptor from vector registers makes every load a loop)
-        const int there = __builtin_amdgcn_readfirstlane(max(0, min(all_pieces - first, W_STEP + TH)));
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.packed + int64_t(first) * piece_bytes), 0, there * piece_bytes, RSRC);
+    auto rows_of = [&](const Place& p) { return int(min(a.tokens - int64_t(p.row_tile) * S::BM, int64_t(S::BM))); };
+    auto tokens_rsrc = [&](const Place& p) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.codes + int64_t(p.row_tile) * S::BM * a.code_stride), 0, rows_of(p) * code_stride, RSRC);
     };
-    const __amdgpu_buffer_rsrc_t rb0 = weight_rsrc(first0), rb1 = weight_rsrc(first1);
-    const int fb0 = first0 >> 3, fb1 = FORM == GEMM_GATED ? first1 >> 3 : fb0 + 1;               // the tile's blocks of features
+    auto scales_rsrc = [&](const Place& p) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.scales + int64_t(p.row_tile) * S::BM * a.scale_stride), 0, rows_of(p) * scale_stride, RSRC);
+    };
+    // pieces of the two feature halves: wave column w, fragment j of half 0 or 1 is piece first(half) + w * W_STEP + j
+    constexpr int W_STEP = FORM == GEMM_GATED ? TH : TN;
+    auto first = [&](const Place& p, int half) { return p.col_tile * (FORM == GEMM_GATED ? TN : 2 * TN) + (half ? (FORM == GEMM_GATED ? a.f_pieces : TH) : 0); };
+    auto weight_rsrc = [&](const Place& p, int half) {
+        // (a clamp is a vector instruction, and a descriptor from vector registers makes every load a loop)
+        const int there = __builtin_amdgcn_readfirstlane(max(0, min(all_pieces - first(p, half), W_STEP + TH)));
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.packed + int64_t(first(p, half)) * piece_bytes), 0, there * piece_bytes, RSRC);
+    };
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.w_scales), 0, (all_pieces >> 3) * a.w_scale_stride, RSRC);
 
     // a load of tokens covers 8 rows x 128 bytes (lane l fills position l % 8 of row l / 8), one of features half a piece. The waves share a
@@ -106,25 +114,44 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     const int vb = pair * W_STEP * piece_bytes + part * 1024 + lane * 16;
     const int lds_a = (pair * TM * 16 + part * 8) * kBlock, lds_b = S::A_BYTES + pair * TN * 2048 + part * 1024;
     // (tiles past the range: the last one once more, into a stage that is not read again)
-    auto load_a = [&](int i, int at, unsigned char* s) {                        // at: K tile in memory
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_t*)(s + lds_a + i * 2048), 16, va + i * 16 * code_stride, at * kBlock, 0, 0);
+    auto load_a = [&](__amdgpu_buffer_rsrc_t r, int i, int at, unsigned char* s) {                        // at: K tile in memory
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t*)(s + lds_a + i * 2048), 16, va + i * 16 * code_stride, at * kBlock, 0, 0);
     };
-    auto load_b = [&](int j, int at, unsigned char* s) {                        // j: fragment 0 .. TN - 1
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(j < TH ? rb0 : rb1, (lds_t*)(s + lds_b + j * 2048), 16,
-                                                 vb + (j < TH ? j : j - TH) * piece_bytes, at * 2048, 0, 0);
+    auto load_b = [&](__amdgpu_buffer_rsrc_t r, int j, int at, unsigned char* s) {                        // j: fragment 0 .. TN - 1, r of its half
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t*)(s + lds_b + j * 2048), 16, vb + (j < TH ? j : j - TH) * piece_bytes, at * 2048, 0, 0);
     };
-    const int last = kt0 + nk - 1;
     // scale words of four tiles: 64 rows to a load, then the two feature blocks (even and odd lanes). Every wave issues as many.
     constexpr int ROW_LOADS = S::SCALE_ROWS / 64, SCALE_LOADS = (ROW_LOADS + 1 + 3) / 4;
-    auto load_scales = [&](int group, unsigned char* s) {
-        const int word = min((kt0 >> 2) + group, last >> 2);
+    auto load_scales = [&](__amdgpu_buffer_rsrc_t r, const Place& p, int word, unsigned char* s) {
+        const int fb0 = first(p, 0) >> 3, fb1 = FORM == GEMM_GATED ? first(p, 1) >> 3 : fb0 + 1;          // the tile's blocks of features
 #pragma unroll
         for (int q = 0; q < SCALE_LOADS; ++q) {
             const int n = min(wave + 4 * q, ROW_LOADS);
             if (n < ROW_LOADS)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(s + n * 256), 4, (n * 64 + lane) * scale_stride, word * 4, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t*)(s + n * 256), 4, (n * 64 + lane) * scale_stride, word * 4, 0, 0);
             else
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_t*)(s + n * 256), 4, (lane & 1 ? fb1 : fb0) * a.w_scale_stride, word * 4, 0, 0);
+        }
+    };
+    constexpr int LA = LO + TH, LB = HI + TH;
+    unsigned char* const scale_lds = smem + NS * S::STAGE;
+    // the first group's scales, then the stages in the order in which they are waited for
+    auto begin = [&](const Place& p) {
+        const __amdgpu_buffer_rsrc_t ra = tokens_rsrc(p), rb0 = weight_rsrc(p, 0), rb1 = weight_rsrc(p, 1);
+        const int kt0 = p.split * g.ktiles_per_split, last = min(a.k_blocks, kt0 + g.ktiles_per_split) - 1;
+        load_scales(scales_rsrc(p), p, kt0 >> 2, scale_lds);
+#pragma unroll
+        for (int q = 0; q < NS; ++q) {
+            unsigned char* s = smem + q * S::STAGE;
+            const int at = min(kt0 + q, last);
+#pragma unroll
+            for (int i = 0; i < LO; ++i) load_a(ra, i, at, s);
+#pragma unroll
+            for (int j = 0; j < TH; ++j) load_b(q & 1 ? rb1 : rb0, q & 1 ? TH + j : j, at, s);
+#pragma unroll
+            for (int i = LO; i < TM; ++i) load_a(ra, i, at, s);
+#pragma unroll
+            for (int j = 0; j < TH; ++j) load_b(q & 1 ? rb0 : rb1, q & 1 ? j : TH + j, at, s);
         }
     };
 
@@ -143,7 +170,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         const int which = FORM == GEMM_GATED ? q : (wn * TN) >> 3;
         to[q] = *reinterpret_cast<const unsigned*>(s + S::SCALE_ROWS * 4 + which * 4);
     };
-    unsigned char* const scale_lds = smem + NS * S::STAGE;
+
+    Place place = place_of(item);
+    begin(place);
+    for (;;) {
+    const int kt0 = place.split * g.ktiles_per_split, nk = min(a.k_blocks, kt0 + g.ktiles_per_split) - kt0, last = kt0 + nk - 1;
+    const __amdgpu_buffer_rsrc_t ra = tokens_rsrc(place), rs = scales_rsrc(place), rb0 = weight_rsrc(place, 0), rb1 = weight_rsrc(place, 1);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -152,23 +184,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             for (int v = 0; v < 4; ++v) acc[i][j][v] = 0.f;
             asm volatile("" : "+a"(acc[i][j]));
         }
-
-    // prologue: the first group's scales, then the stages in the order in which they are waited for
-    constexpr int LA = LO + TH, LB = HI + TH;
-    load_scales(0, scale_lds);
-#pragma unroll
-    for (int q = 0; q < NS; ++q) {
-        unsigned char* s = smem + q * S::STAGE;
-#pragma unroll
-        for (int i = 0; i < LO; ++i) load_a(i, min(kt0 + q, last), s);
-#pragma unroll
-        for (int j = 0; j < TH; ++j) load_b(q & 1 ? TH + j : j, min(kt0 + q, last), s);
-#pragma unroll
-        for (int i = LO; i < TM; ++i) load_a(i, min(kt0 + q, last), s);
-#pragma unroll
-        for (int j = 0; j < TH; ++j) load_b(q & 1 ? j : TH + j, min(kt0 + q, last), s);
-    }
-    wait_vmcnt<(NS - 1) * (LA + LB)>();          // the first tile and the scales have landed
+    // The first K tile and the scales have landed. (Behind them the tile before stored its results: vector memory operations are counted in
+    // order, so this and the next waits are for those stores too. A count that left them out would have to differ in a workgroup's first K
+    // tiles, and a branch there lets the compiler move MFMAs out of the places they are dealt to: 1.38 us a K tile instead of 1.26.)
+    wait_vmcnt<(NS - 1) * (LA + LB)>();
     __builtin_amdgcn_s_barrier();
 #pragma unroll
     for (int i = 0; i < LO; ++i) {
@@ -237,10 +256,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
 #pragma unroll
             for (int l = 0; l < L; ++l)
                 if (l * BAR / L == q) {
-                    if (l < NA) load_a(I0 + l, at, s);
-                    else load_b((HALF ? Y : X) + l - NA, at, s);
+                    if (l < NA) load_a(ra, I0 + l, at, s);
+                    else load_b((HALF ? Y : X) ? rb1 : rb0, (HALF ? Y : X) + l - NA, at, s);
                 }
-            if constexpr (HALF == 0 && IDX == 0 && q == 0) load_scales((kt >> 2) + 1, sc_next);
+            if constexpr (HALF == 0 && IDX == 0 && q == 0) load_scales(rs, place, min((kt0 + kt + 4) >> 2, last >> 2), sc_next);
             __builtin_amdgcn_sched_barrier(0);
         };
         for_constants(slot, std::make_integer_sequence<int, NM>());
@@ -273,13 +292,28 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
 #pragma unroll
             for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
     }
-    wait_vmcnt<0>();                                 // no load into LDS outlives the workgroup
+    __builtin_amdgcn_s_waitcnt(0xC07F);              // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();                    // all waves have read what they read of LDS
+    const Place done = place;
+    item += step_item;
+    const bool more = item < end_item;
+    if (more) {
+        place = place_of(item);
+        begin(place);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 
-    // lane: token l % 16 of fragment i, features 4 * (l / 16) .. + 3 of fragment j
-    const int64_t token0 = row0 + wm * TM * 16 + r;
+    // lane: token l % 16 of fragment i, features 4 * (l / 16) .. + 3 of fragment j. (The offsets of the stores are the same for each of a
+    // workgroup's tiles; made from what the compiler cannot know to be, they take no registers while the next one is computed.)
+    int lane_now = lane;
+    asm volatile("" : "+v"(lane_now));
+    const int row16 = lane_now & 15, quarter = lane_now >> 4;
+    const int64_t row0 = int64_t(done.row_tile) * S::BM;
+    const int tile_rows = rows_of(done), col_tile = done.col_tile;
+    const int64_t token0 = row0 + wm * TM * 16 + row16;
     if constexpr (FORM == GEMM_GATED) {
-        __builtin_amdgcn_s_barrier();
-        unsigned* top = reinterpret_cast<unsigned*>(smem);               // [wave column][token]
+        constexpr unsigned OUT = 0x80000000u;        // out of bounds: not stored
+        unsigned* top = reinterpret_cast<unsigned*>(smem + NS * S::STAGE + 2 * S::SCALES);               // [wave column][token]
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -293,12 +327,17 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             }
             m = max(m, unsigned(__shfl_xor(int(m), 16)));
             m = max(m, unsigned(__shfl_xor(int(m), 32)));
-            if (lane < 16) top[wn * S::BM + wm * TM * 16 + i * 16 + lane] = m;
+            if (lane_now < 16) top[wn * S::BM + wm * TM * 16 + i * 16 + lane_now] = m;
         }
-        __syncthreads();
+        __builtin_amdgcn_s_waitcnt(0xC07F);          // (no __syncthreads(): it would wait for the next tile's loads)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(a.out_codes + row0 * a.out_code_stride + col_tile * kBlock, 0, 0x7fffffff, RSRC);
+        const __amdgpu_buffer_rsrc_t re = __builtin_amdgcn_make_buffer_rsrc(a.out_scales + row0 * a.out_scale_stride, 0, 0x7fffffff, RSRC);
+        const int out_stride = int(a.out_code_stride), out_scale_stride = int(a.out_scale_stride);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const int row = wm * TM * 16 + i * 16 + r;
+            const int row = wm * TM * 16 + i * 16 + row16;
             const unsigned byte = scale_byte(max(top[row], top[S::BM + row]));
             const float inv = inverse_scale(byte);
             unsigned d[4];
@@ -307,29 +346,30 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             // 4 x 4 words between the four rows of lanes: row q ends up with the 16 features of fragment q
             const auto u = __builtin_amdgcn_permlane32_swap(d[0], d[2], false, false), v = __builtin_amdgcn_permlane32_swap(d[1], d[3], false, false);
             const auto lo = __builtin_amdgcn_permlane16_swap(u[0], v[0], false, false), hi = __builtin_amdgcn_permlane16_swap(u[1], v[1], false, false);
+            const bool there = row < tile_rows;
+            const uintx4 o = {lo[0], lo[1], hi[0], hi[1]};
+            __builtin_amdgcn_raw_buffer_store_b128(o, rc, int(there ? unsigned(row * out_stride + wn * 64 + quarter * 16) : OUT), 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b8(static_cast<unsigned char>(byte), re, int(there && wn == 0 && quarter == 0 ? unsigned(row * out_scale_stride + col_tile) : OUT), 0, 0);
+            if (col_tile == 0 && a.spare)
+                __builtin_amdgcn_raw_buffer_store_b8(0, re, int(there && wn == 0 && quarter < a.spare ? unsigned(row * out_scale_stride + (a.f_pieces >> 3) + quarter) : OUT), 0, 0);
+        }
+    } else if constexpr (FORM == GEMM_PARTIAL) {
+        const int piece0 = first(done, 0) + wn * TN;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
             const int64_t token = token0 + i * 16;
+            float* p = a.partial + (int64_t(done.split) * a.tokens + token) * a.ld + piece0 * 16 + quarter * 4;
+#pragma unroll
+            for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
+            __builtin_amdgcn_sched_barrier(0);
             if (token < a.tokens) {
-                *reinterpret_cast<uint4*>(a.out_codes + token * a.out_code_stride + col_tile * kBlock + wn * 64 + kq * 16) = make_uint4(lo[0], lo[1], hi[0], hi[1]);
-                unsigned char* scales = a.out_scales + token * a.out_scale_stride;
-                if (wn == 0 && kq == 0) scales[col_tile] = static_cast<unsigned char>(byte);
-                if (wn == 0 && col_tile == 0 && kq < a.spare) scales[(a.f_pieces >> 3) + kq] = 0;
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    if (piece0 + j < all_pieces) *reinterpret_cast<floatx4*>(p + j * 16) = acc[i][j];
             }
         }
     } else {
-        const int piece0 = first0 + wn * TN;
-        if (a.partial) {
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int64_t token = token0 + i * 16;
-                float* p = a.partial + (int64_t(split) * a.tokens + token) * a.ld + piece0 * 16 + kq * 4;
-                if (token < a.tokens) {
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        if (piece0 + j < all_pieces) *reinterpret_cast<floatx4*>(p + j * 16) = acc[i][j];
-                }
-            }
-            return;
-        }
+        const int piece0 = first(done, 0) + wn * TN;
         // two neighbouring fragments: two lane swaps make 8 consecutive features of a token, 64 bytes of each row at a time
         auto pack = [](float u, float v) {
             typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -338,18 +378,20 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             h[1] = bf16_t(v);
             return __builtin_bit_cast(unsigned, h);
         };
-        const int in32 = 16 * (lane >> 5) + 8 * ((lane >> 4) & 1);
-        int tensor[TH], feature[TH];
+        const int in32 = 16 * (lane_now >> 5) + 8 * ((lane_now >> 4) & 1);
+        // a run of 32 features is within one tensor: where it goes, and how many of its features there are, is the same for the wave
+        int col[TH], left[TH];
 #pragma unroll
-        for (int j = 0; j < TH; ++j) {               // a run of 32 features is within one tensor
-            const int piece = piece0 + 2 * j;
-            tensor[j] = piece / a.f_pieces;
-            feature[j] = (piece - tensor[j] * a.f_pieces) * 16 + in32;
+        for (int j = 0; j < TH; ++j) {
+            const int piece = piece0 + 2 * j, tensor = piece / a.f_pieces, feature = (piece - tensor * a.f_pieces) * 16;
+            col[j] = __builtin_amdgcn_readfirstlane(tensor * a.features + feature);
+            left[j] = __builtin_amdgcn_readfirstlane(tensor < a.tensors ? a.features - feature : 0);
         }
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int64_t token = token0 + i * 16;
-            bf16_t* y = static_cast<bf16_t*>(a.y) + token * a.y_stride;
+            const int row = wm * TM * 16 + i * 16 + row16;
+            bf16_t* y = static_cast<bf16_t*>(a.y) + token * a.y_stride + in32;
 #pragma unroll
             for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
             __builtin_amdgcn_sched_barrier(0);
@@ -359,12 +401,12 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
                 const auto s0 = __builtin_amdgcn_permlane32_swap(pack(p[0], p[1]), pack(q[0], q[1]), false, false);
                 const auto s1 = __builtin_amdgcn_permlane32_swap(pack(p[2], p[3]), pack(q[2], q[3]), false, false);
                 const auto t0 = __builtin_amdgcn_permlane16_swap(s0[0], s0[1], false, false), t1 = __builtin_amdgcn_permlane16_swap(s1[0], s1[1], false, false);
-                const unsigned o[4] = {t0[0], t1[0], t0[1], t1[1]};
-                const int n = tensor[j] < a.tensors ? a.features - feature[j] : 0;
-                if (token >= a.tokens || n <= 0) continue;
-                bf16_t* to = y + int64_t(tensor[j]) * a.features + feature[j];
+                const uintx4 o = {t0[0], t1[0], t0[1], t1[1]};
+                const int n = left[j] - in32;
+                if (row >= tile_rows || n <= 0) continue;
+                bf16_t* to = y + col[j];
                 if (n >= 8) {
-                    __builtin_memcpy(to, o, 16);
+                    __builtin_memcpy(to, &o, 16);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
@@ -373,6 +415,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             }
         }
     }
+    if (!more) break;
+    }
+    wait_vmcnt<0>();                                 // no load into LDS outlives the workgroup
 }
 #endif
 

@@ -173,7 +173,7 @@ struct Choice {
     double us = 1e30;
 };
 
-constexpr int tiles_per_cu(const TileCost& t) {
+constexpr int tiles_per_cu(const TileCost& t) {          // as GemmShape has it
     const int stage = 32 * (t.tm + t.tn) * kBlock, scales = ((32 * t.tm + 63) / 64 * 64 + 64) * 4;
     return 2 * (2 * stage + 2 * scales) <= 160 * 1024 ? 2 : 1;
 }
@@ -247,7 +247,8 @@ int run_gemm(const LinearArgs& a, hipStream_t stream) {
     if (items > INT32_MAX / 8) return TN_ERR_UNSUPPORTED;
     g.n_row = int(n_row);
     g.n_col = int(n_col);
-    gemm_kernel<TM, TN, FORM><<<dim3(unsigned(div_up(items, 8) * 8)), dim3(256), S::SMEM, stream>>>(g);
+    const int64_t held = kCUs * S::PER_CU, groups = div_up(items, 8) * 8;
+    gemm_kernel<TM, TN, FORM><<<dim3(unsigned(groups < held ? groups : held)), dim3(256), S::SMEM, stream>>>(g);
     return launched();
 }
 template <int TM, int TN, int FORM>
@@ -277,7 +278,8 @@ int run_product(const tn_fp8_linear_s& h, LinearArgs a, bool gated, hipStream_t 
     } else if (c.fused) {
         rc = run_tile<GEMM_GATED>(a, c.tile, stream, std::make_integer_sequence<int, kGatedTiles>());
     } else {
-        rc = run_tile<GEMM_PLAIN>(a, c.tile, stream, std::make_integer_sequence<int, kTileCount>());
+        rc = in_parts ? run_tile<GEMM_PARTIAL>(a, c.tile, stream, std::make_integer_sequence<int, kTileCount>())
+                      : run_tile<GEMM_PLAIN>(a, c.tile, stream, std::make_integer_sequence<int, kTileCount>());
     }
     if (rc != TN_OK || !in_parts) return rc;
     const int64_t ktiles = div_up(div_up(a.k_blocks, a.n_split), 4) * 4;
@@ -468,7 +470,7 @@ int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
     h->packed_bytes = int64_t(h->out_segments) * h->f_blocks * 8 * h->k_blocks * 2048;
     h->scale_bytes = int64_t(h->out_segments) * h->f_blocks * h->scale_stride;
     const hipStream_t st = static_cast<hipStream_t>(d->stream);
-    int rc = allow_gemms<GEMM_PLAIN>(std::make_integer_sequence<int, kTileCount>()) && allow_gemms<GEMM_GATED>(std::make_integer_sequence<int, kGatedTiles>()) ? TN_OK : TN_ERR_HIP;
+    int rc = allow_gemms<GEMM_PLAIN>(std::make_integer_sequence<int, kTileCount>()) && allow_gemms<GEMM_PARTIAL>(std::make_integer_sequence<int, kTileCount>()) && allow_gemms<GEMM_GATED>(std::make_integer_sequence<int, kGatedTiles>()) ? TN_OK : TN_ERR_HIP;
     if (rc == TN_OK && (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
         hipMalloc(reinterpret_cast<void**>(&h->scales), size_t(h->scale_bytes)) != hipSuccess)) {
         (void)hipGetLastError();
