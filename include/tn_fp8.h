@@ -142,6 +142,17 @@ int tn_fp8_linear_forward(tn_fp8_linear_t h, const void* codes, const void* scal
 int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales, void* out_codes, void* out_scales, int64_t tokens,
                         void* stream);
 
+/*
+ * Host only, no GPU call, no tensor read (desc->tensors may be NULL): how a call of tn_fp8_linear_forward (gated = 0) or tn_fp8_linear_gated (1) with
+ * `tokens` tokens would run. For the library's own tests and measurements.
+ */
+#define TN_FP8_PLAN_TILE_TOKENS   0   /* tokens of a tile; 0: the weight is streamed, 16 tokens at a time */
+#define TN_FP8_PLAN_TILE_FEATURES 1   /* features of a tile; 0 likewise */
+#define TN_FP8_PLAN_RANGES        2   /* ranges that the inputs are split into, partial sums in the workspace */
+#define TN_FP8_PLAN_FUSED         3   /* gated: silu(gate) * up within the product's launch */
+#define TN_FP8_PLAN_STREAM_PIECES 4   /* streamed: runs of 16 features to a workgroup, else 0 */
+int tn_fp8_linear_plan_query(const tn_fp8_linear_desc* desc, int64_t tokens, int32_t gated, int32_t what, int64_t* value);
+
 /* Codes [M, N] and scale bytes [ceil(M / 128), ceil(N / 128)] of tensor `slot`, as the description takes them (also from a
  * handle made with TN_FLAG_TRANSPOSE). Either pointer may be NULL. */
 int tn_fp8_linear_tensor(tn_fp8_linear_t h, int32_t slot, void* codes, void* scales, void* stream);

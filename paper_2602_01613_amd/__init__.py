@@ -42,6 +42,8 @@ from .fp8 import (  # noqa: F401
     RowOutput,
     TN_DTYPE_FP8,
     TN_FP8_BLOCK,
+    TN_FP8_PLAN_FUSED, TN_FP8_PLAN_RANGES, TN_FP8_PLAN_STREAM_PIECES, TN_FP8_PLAN_TILE_FEATURES, TN_FP8_PLAN_TILE_TOKENS,
+    fp8_plan_query,
     quantize_fp8,
     rms_norm,
     rms_norm_gradients,

@@ -18,7 +18,7 @@ namespace {
 
 constexpr int64_t kMaxRows = int64_t(1) << 30;
 constexpr int64_t kMaxCols = int64_t(1) << 24;
-constexpr int64_t kOwnWorkspace = int64_t(64) << 20;
+constexpr int64_t kOwnWorkspace = int64_t(64) << 20, kMostRanges = 16;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -110,6 +110,35 @@ struct tn_fp8_linear_s {
 };
 
 namespace {
+
+// What a description says by itself, tensors apart
+int check_desc(const tn_fp8_linear_desc& d) {
+    if (d.out_features < 1 || d.in_features < 1 || d.max_tokens < 1 || d.n_tensors < 1 || d.n_tensors > 2 || (d.flags & ~TN_FLAG_TRANSPOSE))
+        return TN_ERR_INVALID_ARG;
+    if (d.dtype != TN_DTYPE_FP8 && !float_type(d.dtype)) return TN_ERR_INVALID_ARG;
+    if (d.workspace ? d.workspace_bytes < 1 || !aligned(d.workspace, 256) : d.workspace_bytes != 0) return TN_ERR_INVALID_ARG;
+    return d.out_features > TN_FP8_MAX_FEATURES || d.in_features > TN_FP8_MAX_FEATURES || d.max_tokens > kMaxRows ? TN_ERR_UNSUPPORTED : TN_OK;
+}
+
+// sizes of the operand and of the workspace
+void lay_out(const tn_fp8_linear_desc& d, tn_fp8_linear_s& h) {
+    h.tensors = d.n_tensors;
+    h.transpose = (d.flags & TN_FLAG_TRANSPOSE) ? 1 : 0;
+    h.m = d.out_features;
+    h.n = d.in_features;
+    h.features = int32_t(h.transpose ? h.n : h.m);
+    h.f_blocks = int32_t(div_up(h.features, kBlock));
+    h.out_segments = h.transpose ? 1 : h.tensors;
+    h.k_cols = int32_t(h.transpose ? h.m : h.n);
+    h.k_segments = h.transpose ? h.tensors : 1;
+    h.k_blocks = int32_t(h.k_segments * div_up(h.k_cols, kBlock));
+    h.scale_stride = int32_t(div_up(h.k_blocks, 4) * 4);
+    h.packed_bytes = int64_t(h.out_segments) * h.f_blocks * 8 * h.k_blocks * 2048;
+    h.scale_bytes = int64_t(h.out_segments) * h.f_blocks * h.scale_stride;
+    // the most ranges of K there are, at max_tokens: more than the products ask for, and no more than 64 MB
+    const int64_t want = div_up(kMostRanges * d.max_tokens * h.out_segments * h.f_blocks * kBlock * 4, 256) * 256;
+    h.workspace_bytes = d.workspace ? d.workspace_bytes : want < kOwnWorkspace ? want : kOwnWorkspace;
+}
 
 WeightArgs weight_args(const tn_fp8_linear_s& h, int slot) {
     WeightArgs a{};
@@ -446,29 +475,16 @@ int tn_silu_gate_gradients(int32_t dtype, int64_t rows, int64_t cols, const void
 }
 
 int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
-    if (!out || !d || !d->tensors || d->out_features < 1 || d->in_features < 1 || d->max_tokens < 1) return TN_ERR_INVALID_ARG;
-    if (d->workspace ? d->workspace_bytes < 1 || !aligned(d->workspace, 256) : d->workspace_bytes != 0) return TN_ERR_INVALID_ARG;
+    if (!out || !d || !d->tensors) return TN_ERR_INVALID_ARG;
     const bool given = d->dtype == TN_DTYPE_FP8;
-    if ((!given && !float_type(d->dtype)) || (given && !d->scales) || d->n_tensors < 1 || d->n_tensors > 2 || (d->flags & ~TN_FLAG_TRANSPOSE))
-        return TN_ERR_INVALID_ARG;
-    if (d->out_features > TN_FP8_MAX_FEATURES || d->in_features > TN_FP8_MAX_FEATURES || d->max_tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    const int bad = check_desc(*d);
+    if (bad != TN_OK) return bad;
+    if (given && !d->scales) return TN_ERR_INVALID_ARG;
     for (int i = 0; i < d->n_tensors; ++i)
         if (!d->tensors[i] || (given && !d->scales[i]) || (!given && !aligned(d->tensors[i], unsigned(element_bytes(d->dtype))))) return TN_ERR_INVALID_ARG;
     tn_fp8_linear_s* h = new (std::nothrow) tn_fp8_linear_s;
     if (!h) return TN_ERR_ALLOC;
-    h->tensors = d->n_tensors;
-    h->transpose = (d->flags & TN_FLAG_TRANSPOSE) ? 1 : 0;
-    h->m = d->out_features;
-    h->n = d->in_features;
-    h->features = int32_t(h->transpose ? h->n : h->m);
-    h->f_blocks = int32_t(div_up(h->features, kBlock));
-    h->out_segments = h->transpose ? 1 : h->tensors;
-    h->k_cols = int32_t(h->transpose ? h->m : h->n);
-    h->k_segments = h->transpose ? h->tensors : 1;
-    h->k_blocks = int32_t(h->k_segments * div_up(h->k_cols, kBlock));
-    h->scale_stride = int32_t(div_up(h->k_blocks, 4) * 4);
-    h->packed_bytes = int64_t(h->out_segments) * h->f_blocks * 8 * h->k_blocks * 2048;
-    h->scale_bytes = int64_t(h->out_segments) * h->f_blocks * h->scale_stride;
+    lay_out(*d, *h);
     const hipStream_t st = static_cast<hipStream_t>(d->stream);
     int rc = allow_gemms<GEMM_PLAIN>(std::make_integer_sequence<int, kTileCount>()) && allow_gemms<GEMM_PARTIAL>(std::make_integer_sequence<int, kTileCount>()) && allow_gemms<GEMM_GATED>(std::make_integer_sequence<int, kGatedTiles>()) ? TN_OK : TN_ERR_HIP;
     if (rc == TN_OK && (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
@@ -478,11 +494,7 @@ int tn_fp8_linear_create(tn_fp8_linear_t* out, const tn_fp8_linear_desc* d) {
     }
     if (d->workspace) {
         h->workspace = d->workspace;
-        h->workspace_bytes = d->workspace_bytes;
     } else if (rc == TN_OK) {
-        // the most ranges of K there are, at max_tokens: more than the products ask for, and no more than 64 MB
-        const int64_t want = div_up(16 * d->max_tokens * h->out_segments * h->f_blocks * kBlock * 4, 256) * 256;
-        h->workspace_bytes = want < kOwnWorkspace ? want : kOwnWorkspace;
         h->own_workspace = true;
         if (hipMalloc(&h->workspace, size_t(h->workspace_bytes)) != hipSuccess) {
             (void)hipGetLastError();
@@ -533,6 +545,26 @@ int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales
     a.out_scale_stride = o.scale_stride;
     a.spare = o.spare;
     return run_product(*h, a, true, static_cast<hipStream_t>(stream));
+}
+
+int tn_fp8_linear_plan_query(const tn_fp8_linear_desc* d, int64_t tokens, int32_t gated, int32_t what, int64_t* value) {
+    if (!d || !value || tokens < 1 || (gated && (d->n_tensors != 2 || (d->flags & TN_FLAG_TRANSPOSE)))) return TN_ERR_INVALID_ARG;
+    const int bad = check_desc(*d);
+    if (bad != TN_OK) return bad;
+    if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    tn_fp8_linear_s h;
+    lay_out(*d, h);
+    const LinearArgs a = linear_args(h, nullptr, nullptr, tokens);
+    const Choice c = choose(a, gated != 0, h.workspace_bytes);
+    const TileCost tile = c.tile < 0 ? TileCost{} : kTiles[c.tile];
+    switch (what) {
+        case TN_FP8_PLAN_TILE_TOKENS: *value = 32 * tile.tm; return TN_OK;
+        case TN_FP8_PLAN_TILE_FEATURES: *value = 32 * tile.tn; return TN_OK;
+        case TN_FP8_PLAN_RANGES: *value = c.split; return TN_OK;
+        case TN_FP8_PLAN_FUSED: *value = c.fused ? 1 : 0; return TN_OK;
+        case TN_FP8_PLAN_STREAM_PIECES: *value = c.tile < 0 ? c.groups : 0; return TN_OK;
+        default: return TN_ERR_INVALID_ARG;
+    }
 }
 
 int tn_fp8_linear_tensor(tn_fp8_linear_t h, int32_t slot, void* codes, void* scales, void* stream) {

@@ -32,6 +32,7 @@ FP8_EXPORTED_SYMBOLS = (
     "tn_fp8_linear_create",
     "tn_fp8_linear_forward",
     "tn_fp8_linear_gated",
+    "tn_fp8_linear_plan_query",
     "tn_fp8_linear_tensor",
     "tn_fp8_linear_query",
     "tn_fp8_linear_destroy",
@@ -76,6 +77,7 @@ def _library():
             "tn_fp8_linear_create": [ctypes.POINTER(p), ctypes.POINTER(_Desc)],
             "tn_fp8_linear_forward": [p, p, p, p, i64, i64, p],
             "tn_fp8_linear_gated": [p, p, p, p, p, i64, p],
+            "tn_fp8_linear_plan_query": [ctypes.POINTER(_Desc), i64, i32, i32, ctypes.POINTER(i64)],
             "tn_fp8_linear_tensor": [p, i32, p, p, p],
             "tn_fp8_linear_query": [p, i32, ctypes.POINTER(i64)],
             "tn_fp8_linear_destroy": [p],
@@ -137,7 +139,7 @@ class Fp8Rows:
     [rows, S], one for each block of 128, S rounded up to 4), as include/tn_fp8.h lays them out. `values` and `block_scales`
     are views of a segment without its padding."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "segments")
+    __slots__ = ("codes", "scales", "rows", "cols", "segments", "_parts")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, cols: int, segments: int = 1):
         width, blocks = -(-cols // TN_FP8_BLOCK) * TN_FP8_BLOCK * segments, -(-cols // TN_FP8_BLOCK) * segments
@@ -146,7 +148,7 @@ class Fp8Rows:
             raise ValueError(f"codes must be a contiguous CUDA [rows, {width}] tensor of float8_e4m3fn")
         if not (scales.is_cuda and scales.dtype == _SCALES and scales.is_contiguous() and tuple(scales.shape) == (rows, -(-blocks // 4) * 4)):
             raise ValueError(f"scales must be a contiguous CUDA [{rows}, {-(-blocks // 4) * 4}] tensor of float8_e8m0fnu")
-        self.codes, self.scales, self.rows, self.cols, self.segments = codes, scales, rows, cols, segments
+        self.codes, self.scales, self.rows, self.cols, self.segments, self._parts = codes, scales, rows, cols, segments, None
 
     @classmethod
     def empty(cls, rows: int, cols: int, segments: int = 1, device="cuda") -> "Fp8Rows":
@@ -154,19 +156,29 @@ class Fp8Rows:
         new = cls.__new__(cls)
         new.codes = torch.empty((rows, blocks * TN_FP8_BLOCK), dtype=_CODES, device=device)
         new.scales = torch.empty((rows, -(-blocks // 4) * 4), dtype=_SCALES, device=device)
-        new.rows, new.cols, new.segments = rows, cols, segments
+        new.rows, new.cols, new.segments, new._parts = rows, cols, segments, None
         return new
 
+    def _segment(self, segment: int):
+        """(codes, scales) of a segment: views, made once for all segments (a view costs as much as a tenth of a small call)."""
+        parts = self._parts
+        if parts is None:
+            cols, segments, blocks = self.cols, self.segments, -(-self.cols // TN_FP8_BLOCK)
+            codes, scales = self.codes, self.scales
+            codes = codes.split(blocks * TN_FP8_BLOCK, 1) if segments > 1 else (codes,)
+            if cols % TN_FP8_BLOCK:
+                codes = [c.narrow(1, 0, cols) for c in codes]
+            if scales.shape[1] != blocks * segments:
+                scales = scales.narrow(1, 0, blocks * segments)
+            scales = scales.split(blocks, 1) if segments > 1 else (scales,)
+            parts = self._parts = (codes, scales)
+        return parts[0][segment], parts[1][segment]
+
     def values(self, segment: int = 0) -> torch.Tensor:
-        if self.codes.shape[1] == self.cols:
-            return self.codes
-        return self.codes.narrow(1, segment * (-(-self.cols // TN_FP8_BLOCK) * TN_FP8_BLOCK), self.cols)
+        return self._segment(segment)[0]
 
     def block_scales(self, segment: int = 0) -> torch.Tensor:
-        blocks = -(-self.cols // TN_FP8_BLOCK)
-        if self.scales.shape[1] == blocks:
-            return self.scales
-        return self.scales.narrow(1, segment * blocks, blocks)
+        return self._segment(segment)[1]
 
     def _ready(self, name: str, rows: int, cols: int, segments: int) -> "Fp8Rows":
         if (self.rows, self.cols, self.segments) != (rows, cols, segments):
@@ -286,6 +298,20 @@ def silu_gate_gradients(gate_up: torch.Tensor, dh: torch.Tensor, outputs: str = 
                                              fp8.codes.data_ptr() if fp8 else None, fp8.scales.data_ptr() if fp8 else None, _stream()),
            "tn_silu_gate_gradients")
     return RowOutput(y, fp8)
+
+
+TN_FP8_PLAN_TILE_TOKENS, TN_FP8_PLAN_TILE_FEATURES, TN_FP8_PLAN_RANGES, TN_FP8_PLAN_FUSED, TN_FP8_PLAN_STREAM_PIECES = range(5)
+
+
+def fp8_plan_query(out_features: int, in_features: int, n_tensors: int, tokens: int, gated: bool, what: int, transpose: bool = False,
+                   max_tokens: Optional[int] = None) -> int:
+    """Host-only: how a call of such a layer would run (TN_FP8_PLAN_*); needs no GPU."""
+    desc = _Desc()
+    desc.dtype, desc.n_tensors, desc.out_features, desc.in_features = TN_DTYPE_BF16, n_tensors, out_features, in_features
+    desc.max_tokens, desc.flags = tokens if max_tokens is None else max_tokens, TN_FLAG_TRANSPOSE if transpose else 0
+    value = ctypes.c_int64(0)
+    _check(_library().tn_fp8_linear_plan_query(ctypes.byref(desc), tokens, int(gated), what, ctypes.byref(value)), "tn_fp8_linear_plan_query")
+    return int(value.value)
 
 
 class Fp8Linear:

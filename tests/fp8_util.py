@@ -58,3 +58,20 @@ def check_eight_bit(rows8, ref, segment=0, rel=1e-5):
     assert (np.abs(got - ref)[fine] <= bound[fine]).all()
     differ = (codes != ref_codes)[fine].mean() if fine.any() else 0.0
     assert differ <= 2e-3 + 128.5 * (exps != Q.quantize(ref)[1]).sum() / ref.size, differ
+
+
+# (gated, out_features, in_features, tokens): a call of each form a product has - every tile with its own output, with partial sums of
+# ranges and with silu(gate) * up; streamed with each number of pieces - and tiles of which a workgroup takes several
+FORM_CASES = [
+    (0, 100, 100, 1), (0, 4100, 100, 1), (0, 25600, 100, 8),
+    (0, 520, 256, 2048), (0, 520, 100, 4096), (0, 300, 100, 12000), (0, 12000, 2048, 400), (0, 520, 100, 6000), (0, 12000, 4096, 600),
+    (0, 10000, 256, 777), (0, 300, 1000, 12000), (0, 6000, 512, 1700), (0, 10000, 100, 1300), (0, 1500, 2048, 4096), (0, 5120, 100, 3000),
+    (0, 300, 3000, 777), (0, 1500, 5120, 200), (0, 2600, 5120, 80), (0, 6000, 12000, 256), (0, 100, 12000, 4096), (0, 4100, 12000, 600),
+    (0, 3000, 25600, 300), (0, 6000, 8192, 160), (0, 3000, 12000, 1300), (0, 12000, 12000, 200), (0, 300, 25600, 2048), (0, 1500, 25600, 1000),
+    (1, 100, 512, 1), (1, 2600, 512, 1), (1, 8192, 1000, 8),
+    (1, 100, 100, 1), (1, 25600, 256, 80), (1, 520, 1000, 6000), (1, 300, 256, 12000), (1, 520, 512, 8192), (1, 25600, 100, 200), (1, 520, 100, 12000),
+    (1, 100, 3000, 600), (1, 2048, 5120, 24), (1, 520, 8192, 80), (1, 520, 25600, 400), (1, 5120, 3000, 100), (1, 520, 25600, 777),
+    (0, 1500, 100, 4096), (0, 4100, 256, 4096), (0, 2600, 100, 6000), (0, 25600, 4096, 600), (0, 25600, 256, 777), (0, 4100, 1000, 4096),
+    (0, 2600, 512, 8192), (0, 4100, 256, 6000), (0, 2600, 2048, 6000), (0, 10000, 100, 3000),
+    (1, 300, 100, 6000), (1, 12000, 1000, 600), (1, 10000, 1000, 777), (1, 2600, 512, 4096), (1, 16000, 256, 777), (1, 5120, 100, 3000),
+]

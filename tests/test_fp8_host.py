@@ -193,3 +193,40 @@ def test_binding_refuses_host_tensors():
     if not torch.cuda.is_available():
         with pytest.raises(RuntimeError):
             tn.Fp8Linear([x], 1)
+
+
+TILES = [(64, 256), (96, 256), (128, 256), (160, 256), (192, 256), (224, 256), (256, 256), (64, 128), (96, 128), (128, 128), (192, 128), (256, 128)]
+
+
+def test_every_form_of_a_product_is_among_the_tested_sizes():
+    from fp8_util import FORM_CASES
+    seen, several = set(), set()
+    for gated, m, n, tokens in FORM_CASES:
+        ask = lambda what: tn.fp8_plan_query(m, n, 1 + gated, tokens, bool(gated), what)      # noqa: E731
+        tile = (ask(tn.TN_FP8_PLAN_TILE_TOKENS), ask(tn.TN_FP8_PLAN_TILE_FEATURES))
+        ranges, fused, pieces = ask(tn.TN_FP8_PLAN_RANGES), ask(tn.TN_FP8_PLAN_FUSED), ask(tn.TN_FP8_PLAN_STREAM_PIECES)
+        assert (tile == (0, 0)) == (pieces > 0) and ranges >= 1 and not (fused and (ranges > 1 or not gated))
+        kind = "fused" if fused else "partial" if gated or ranges > 1 else "output"
+        seen.add((kind, pieces) if pieces else (kind, tile))
+        if not pieces:
+            blocks = -(-m // 128) * 128 * (1 + gated)
+            items = -(-tokens // tile[0]) * -(-blocks // tile[1]) * ranges
+            if items > 256 * (2 if sum(tile) <= 256 else 1):
+                several.add((kind, tile))
+    want = {("output", t) for t in TILES} | {("partial", t) for t in TILES[:10]} | {("partial", (256, 128)), ("partial", (192, 128))}
+    want |= {("fused", t) for t in TILES[:7]} | {(k, g) for k in ("output", "partial") for g in (1, 2, 4)}
+    assert not want - seen, want - seen
+    assert len({t for k, t in several if k == "output"}) >= 8 and len({t for k, t in several if k == "fused"}) >= 5, several
+
+
+def test_plan_queries_refuse():
+    lib = fp8._library()
+    value = ctypes.c_int64(0)
+    d, keep = _desc(tensors=None, n_tensors=2)
+    ask = lambda tokens=1, gated=0, what=0, desc=d: lib.tn_fp8_linear_plan_query(ctypes.byref(desc) if desc else None, tokens, gated, what, ctypes.byref(value))      # noqa: E731
+    assert ask() == 0 and ask(gated=1) == 0
+    assert ask(tokens=0) == INVALID and ask(what=99) == INVALID and ask(desc=None) == INVALID and ask(tokens=1 << 40) == UNSUPPORTED
+    one, keep1 = _desc(tensors=None)
+    back, keep2 = _desc(tensors=None, n_tensors=2, flags=tn.TN_FLAG_TRANSPOSE)
+    assert ask(gated=1, desc=one) == INVALID and ask(gated=1, desc=back) == INVALID and ask(desc=back) == 0
+    assert lib.tn_fp8_linear_plan_query(ctypes.byref(d), 1, 0, 0, None) == INVALID

@@ -5,7 +5,7 @@ import torch
 
 import oracle.fp8_oracle as Q
 import paper_2602_01613_amd as tn
-from fp8_util import check_eight_bit, check_padding, dev, exponents, half_unit, host, rounded
+from fp8_util import FORM_CASES, check_eight_bit, check_padding, dev, exponents, half_unit, host, rounded
 
 pytestmark = pytest.mark.gpu
 
@@ -258,3 +258,53 @@ def test_binding_refuses():
         layer.quantized_tensor(2)
     with pytest.raises(tn.TNLinearError):
         layer.query(999)
+
+
+def exact_rows(codes, scales, rows=1):
+    """Codes and scales in 64 bits, on the GPU."""
+    n, k = codes.shape
+    scale = scales.contiguous().view(torch.uint8).double().sub(127).exp2()
+    return codes.double() * scale.repeat_interleave(rows, 0)[:n].repeat_interleave(128, 1)[:, :k]
+
+
+def sums_off_gpu(x8, w8):
+    pad = -x8.shape[1] % 8
+    most = lambda v: torch.nn.functional.pad(v.abs(), (0, pad)).reshape(v.shape[0], -1, 8).amax(dim=2)      # noqa: E731
+    return (7 * 2.0 ** -13 + 2.0 ** -18) * (most(x8) @ most(w8).t().contiguous())
+
+
+@pytest.mark.parametrize("gated,m,n,tokens", FORM_CASES)
+def test_every_form(gated, m, n, tokens):
+    """Each kernel a product may take, at sizes that choose it, against 64 bits on the layer's own codes."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(m + n + tokens)
+    weights = [(torch.randn((m, n), generator=gen, device="cuda") / n ** 0.5).bfloat16() for _ in range(1 + gated)]
+    layer = tn.Fp8Linear(weights, tokens)
+    rows = tn.quantize_fp8(torch.randn((tokens, n), generator=gen, device="cuda").bfloat16())
+    x8, w8 = exact_rows(rows.values(), rows.block_scales()), [exact_rows(*layer.quantized_tensor(i), 128) for i in range(1 + gated)]
+    sums, off = [x8 @ w.t() for w in w8], [sums_off_gpu(x8, w) for w in w8]
+    if not gated:
+        y = layer(rows).double()
+        unit = torch.exp2(torch.floor(torch.log2(sums[0].abs().clamp(min=2.0 ** -120))) - 8)          # half a unit in bf16's last place
+        err = (y - sums[0]).abs()
+        assert (err <= 2 * unit + off[0]).all()                                                       # (twice: ref and y may differ in their powers of two)
+        assert err.norm() <= 2.0 ** -8 * sums[0].norm()
+        assert torch.equal(layer(rows).double(), y)
+        return
+    got = layer.gated(rows)
+    check_padding(got)
+    (gate, up), (eg, eu) = sums, off
+    sig = torch.sigmoid(gate)
+    ref = gate * sig * up
+    off = 1.1 * up.abs() * eg + (gate * sig).abs() * eu + 1.1 * eg * eu + 2.0 ** -20 * ref.abs()
+    values = exact_rows(got.values(), got.block_scales())
+    scale = got.block_scales().contiguous().view(torch.uint8).double().sub(127).exp2()
+    wide = scale.repeat_interleave(128, 1)[:, :m]
+    assert ((values - ref).abs() <= 2.0 ** -4 * (ref.abs() + off) + 2.0 ** -10 * wide + off).all()
+    pad = -m % 128
+    most = torch.nn.functional.pad(ref.abs(), (0, pad)).reshape(tokens, -1, 128).amax(dim=2)
+    slack = torch.nn.functional.pad(off, (0, pad)).reshape(tokens, -1, 128).amax(dim=2)
+    assert ((most - slack) <= 448 * scale).all() and ((most + slack) > 224 * scale).all()
+    assert (values - ref).norm() <= 2.0 ** -4 * ref.norm()
+    again = layer.gated(rows)
+    assert torch.equal(again.codes.view(torch.uint8), got.codes.view(torch.uint8)) and torch.equal(again.scales.view(torch.uint8), got.scales.view(torch.uint8))
