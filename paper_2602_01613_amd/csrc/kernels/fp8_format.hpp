@@ -62,17 +62,26 @@ __device__ __forceinline__ unsigned row16_max(unsigned v) {
     return v;
 }
 
-// Sum over the wave, the same in all lanes
-__device__ __forceinline__ float wave_sum(float v) {
+// Sums over a row of 16 lanes and over the wave, the same in all lanes
+__device__ __forceinline__ float row16_sum(float v) {
 #define TN_ROW_ADD(CTRL) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false))
     TN_ROW_ADD(0x128);
     TN_ROW_ADD(0x124);
     TN_ROW_ADD(0x122);
     TN_ROW_ADD(0x121);
 #undef TN_ROW_ADD
+    return v;
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v = row16_sum(v);
     v += __shfl_xor(v, 16);
     v += __shfl_xor(v, 32);
     return v;
+}
+// Sum of the up to 16 waves' parts: one read of LDS, where a loop over them waits for each
+__device__ __forceinline__ float parts_sum(const float* part, int waves) {
+    const int q = threadIdx.x & 15;
+    return row16_sum(q < waves ? part[q] : 0.f);
 }
 
 // 8 elements at p, of which the first n exist (the others are 0), as they are in memory: rows of any alignment the type has.

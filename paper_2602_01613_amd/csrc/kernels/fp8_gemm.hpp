@@ -21,6 +21,7 @@
 struct GemmArgs {
     LinearArgs l;
     int32_t n_row, n_col;            // output tiles
+    int32_t band;                    // rows of tiles to a band
     int32_t ktiles_per_split;        // a multiple of 4; at least one tile in every range
 };
 
@@ -63,8 +64,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
 
-    // XCD x takes a contiguous eighth of the tiles in bands of four token tiles (tokens fastest), so that the 32 tiles that it runs at
-    // a time share 4 + 8 operand panels in its L2. A launch has no more workgroups than the chip holds: each takes every so many of its
+    // XCD x takes a contiguous eighth of the tiles in bands of up to five token tiles (tokens fastest): the 32 tiles that it runs at
+    // a time share 5 + 7 operand panels in its L2, and the weight is read from behind it once a band. A launch has no more workgroups than the chip holds: each takes every so many of its
     // XCD's tiles, and brings the first stages of the next one while it stores this one.
     const int n_items = g.n_row * g.n_col * a.n_split, xcd = blockIdx.x & 7;
     const int end_item = int(int64_t(n_items) * (xcd + 1) >> 3), step_item = gridDim.x >> 3;
@@ -74,14 +75,13 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
         int row_tile, col_tile, split;
     };
     auto place_of = [&](int at) {
-        constexpr int BAND = 4;
         Place p;
         const int tile = at / a.n_split;
         p.split = __builtin_amdgcn_readfirstlane(at - tile * a.n_split);
-        const int band = tile / (BAND * g.n_col), in_band = tile - band * (BAND * g.n_col);
-        const int band_rows = min(BAND, g.n_row - band * BAND);
+        const int band = tile / (g.band * g.n_col), in_band = tile - band * (g.band * g.n_col);
+        const int band_rows = min(g.band, g.n_row - band * g.band);
         p.col_tile = __builtin_amdgcn_readfirstlane(in_band / band_rows);
-        p.row_tile = __builtin_amdgcn_readfirstlane(band * BAND + in_band - p.col_tile * band_rows);
+        p.row_tile = __builtin_amdgcn_readfirstlane(band * g.band + in_band - p.col_tile * band_rows);
         return p;
     };
 

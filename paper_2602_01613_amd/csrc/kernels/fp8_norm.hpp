@@ -54,8 +54,7 @@ __global__ void __launch_bounds__(ONE_WAVE ? 256 : 1024) rms_norm_kernel(NormArg
         __shared__ float part[16];
         if ((tid & 63) == 0) part[tid >> 6] = sq;
         __syncthreads();
-        sq = 0.f;
-        for (int w = 0; w < (threads >> 6); ++w) sq += part[w];
+        sq = parts_sum(part, threads >> 6);
     }
     if (a.sum) {
 #pragma unroll
@@ -142,8 +141,8 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
         dot = wave_sum(dot);
         if ((tid & 63) == 0) part[slot][0][tid >> 6] = sq, part[slot][1][tid >> 6] = dot;
         __syncthreads();                             // one barrier a row: the next row writes the other slots
-        sq = dot = 0.f;
-        for (int q = 0; q < waves; ++q) sq += part[slot][0][q], dot += part[slot][1][q];
+        sq = parts_sum(part[slot][0], waves);
+        dot = parts_sum(part[slot][1], waves);
         const float r = 1.f / sqrtf(sq / float(a.cols) + a.eps);
         const float along = dot * r * (r / float(a.cols));          // mean(g * u) * r
         T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;

@@ -190,6 +190,9 @@ constexpr TileCost kTiles[] = {{2, 8, 0.50, 2.0}, {3, 8, 0.57, 5.0}, {4, 8, 0.72
 constexpr int kTileCount = int(sizeof(kTiles) / sizeof(kTiles[0])), kGatedTiles = 7;
 constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 10, 16};
 constexpr int kCUs = 256;
+// Rows of tiles to a band, at the most. (Gated 777 tokens on 5 rows: 179 us in one band, 185 in bands of 4 and 1, where the weight is read twice; 8192 x 5120 x
+// 25600 on 32 rows: 764 us in bands of 5, 775 in bands of 4 or 8.)
+constexpr int kBand = 5;
 constexpr double kLaunch = 4.0, kReadRate = 5.3e6, kSumsRate = 8e6;      // bytes per us: memory, partial sums
 constexpr double kTilesRate = 25e6, kStreamRate = 14e6, kStreamFarRate = 11e6;       // what is read again, from the caches
 // Memory and computation overlap, but not wholly: of the shorter one this much is added.
@@ -276,6 +279,7 @@ int run_gemm(const LinearArgs& a, hipStream_t stream) {
     if (items > INT32_MAX / 8) return TN_ERR_UNSUPPORTED;
     g.n_row = int(n_row);
     g.n_col = int(n_col);
+    g.band = int(div_up(n_row, div_up(n_row, kBand)));
     const int64_t held = kCUs * S::PER_CU, groups = div_up(items, 8) * 8;
     gemm_kernel<TM, TN, FORM><<<dim3(unsigned(groups < held ? groups : held)), dim3(256), S::SMEM, stream>>>(g);
     return launched();

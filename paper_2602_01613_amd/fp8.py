@@ -197,17 +197,23 @@ _OUTPUTS = {"y": (True, False), "fp8": (False, True), "both": (True, True)}
 
 
 def _outputs(outputs: str, out: Optional[RowOutput], like: torch.Tensor, rows: int, cols: int, segments: int):
-    """(y, fp8, row stride of y) of a call: the caller's, or new ones."""
-    if outputs not in _OUTPUTS:
+    """(y, its address, its row stride, fp8, the addresses of its codes and scales) of a call: the caller's, or new ones."""
+    want = _OUTPUTS.get(outputs)
+    if want is None:
         raise ValueError('outputs is "y", "fp8" or "both"')
-    want_y, want_fp8 = _OUTPUTS[outputs]
-    y, fp8, stride = None, None, 0
-    if want_y:
-        y = out.y if out is not None and out.y is not None else torch.empty((rows, segments * cols), dtype=like.dtype, device=like.device)
-        stride = _matrix("out.y", y, rows, segments * cols, like.dtype)
-    if want_fp8:
+    y, y_ptr, stride, fp8, codes, scales = None, None, 0, None, None, None
+    if want[0]:
+        if out is not None and out.y is not None:
+            y = out.y
+            stride = _matrix("out.y", y, rows, segments * cols, like.dtype)
+        else:
+            stride = segments * cols
+            y = like.new_empty((rows, stride))
+        y_ptr = y.data_ptr()
+    if want[1]:
         fp8 = out.fp8._ready("out.fp8", rows, cols, segments) if out is not None and out.fp8 is not None else Fp8Rows.empty(rows, cols, segments, like.device)
-    return y, fp8, stride
+        codes, scales = fp8.codes.data_ptr(), fp8.scales.data_ptr()
+    return y, y_ptr, stride, fp8, codes, scales
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -236,15 +242,18 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float 
     code = _input("x", x)
     rows, cols = x.shape
     x_stride = _matrix("x", x, rows, cols, x.dtype)
-    y, fp8, y_stride = _outputs(outputs, out, x, rows, cols, 1)
-    total, res_stride, sum_stride = None, 0, 0
+    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, x, rows, cols, 1)
+    total, total_ptr, res_ptr, res_stride, sum_stride = None, None, None, 0, 0
     if residual is not None:
-        res_stride = _matrix("residual", residual, rows, cols, x.dtype)
-        total = out.sum if out is not None and out.sum is not None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-        sum_stride = _matrix("out.sum", total, rows, cols, x.dtype)
-    _check(_library().tn_rms_norm(code, rows, cols, x.data_ptr(), x_stride, _ptr(residual), res_stride, _vector("weight", weight, cols, x.dtype),
-                                  eps, _ptr(total), sum_stride, _ptr(y), y_stride, fp8.codes.data_ptr() if fp8 else None,
-                                  fp8.scales.data_ptr() if fp8 else None, _stream()), "tn_rms_norm")
+        res_stride, res_ptr = _matrix("residual", residual, rows, cols, x.dtype), residual.data_ptr()
+        if out is not None and out.sum is not None:
+            total = out.sum
+            sum_stride = _matrix("out.sum", total, rows, cols, x.dtype)
+        else:
+            total, sum_stride = x.new_empty((rows, cols)), cols
+        total_ptr = total.data_ptr()
+    _check(_library().tn_rms_norm(code, rows, cols, x.data_ptr(), x_stride, res_ptr, res_stride, _vector("weight", weight, cols, x.dtype), eps,
+                                  total_ptr, sum_stride, y_ptr, y_stride, codes, scales, _stream()), "tn_rms_norm")
     return RowOutput(y, fp8, total)
 
 
@@ -260,16 +269,17 @@ def rms_norm_gradients(dy: torch.Tensor, s: torch.Tensor, weight: Optional[torch
     dy_stride = _matrix("dy", dy, rows, cols, s.dtype)
     ds_stride = 0 if dsum is None else _matrix("dsum", dsum, rows, cols, s.dtype)
     if dx is None:
-        dx = torch.empty((rows, cols), dtype=s.dtype, device=s.device)
-    dx_stride = _matrix("dx", dx, rows, cols, s.dtype)
+        dx, dx_stride = s.new_empty((rows, cols)), cols
+    else:
+        dx_stride = _matrix("dx", dx, rows, cols, s.dtype)
     lib = _library()
     dw, space, need = None, None, 0
     if dweight and weight is not None:
         need = lib.tn_rms_norm_gradients_workspace(rows, cols)
         if need < 0:
             _check(int(need), "tn_rms_norm_gradients_workspace")
-        dw = torch.empty((cols,), dtype=torch.float32, device=s.device)
-        space = torch.empty((need,), dtype=torch.uint8, device=s.device)
+        dw = s.new_empty((cols,), dtype=torch.float32)
+        space = s.new_empty((need,), dtype=torch.uint8)
     _check(lib.tn_rms_norm_gradients(code, rows, cols, dy.data_ptr(), dy_stride, s.data_ptr(), s_stride, _vector("weight", weight, cols, s.dtype),
                                      eps, _ptr(dsum), ds_stride, dx.data_ptr(), dx_stride, _ptr(dw), _ptr(space), need, _stream()),
            "tn_rms_norm_gradients")
@@ -281,9 +291,8 @@ def silu_gate(gate_up: torch.Tensor, outputs: str = "y", out: Optional[RowOutput
     code = _input("gate_up", gate_up)
     rows, cols = gate_up.shape[0], gate_up.shape[1] // 2
     stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype)
-    y, fp8, y_stride = _outputs(outputs, out, gate_up, rows, cols, 1)
-    _check(_library().tn_silu_gate(code, rows, cols, gate_up.data_ptr(), stride, _ptr(y), y_stride, fp8.codes.data_ptr() if fp8 else None,
-                                   fp8.scales.data_ptr() if fp8 else None, _stream()), "tn_silu_gate")
+    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, gate_up, rows, cols, 1)
+    _check(_library().tn_silu_gate(code, rows, cols, gate_up.data_ptr(), stride, y_ptr, y_stride, codes, scales, _stream()), "tn_silu_gate")
     return RowOutput(y, fp8)
 
 
@@ -293,10 +302,9 @@ def silu_gate_gradients(gate_up: torch.Tensor, dh: torch.Tensor, outputs: str = 
     rows, cols = gate_up.shape[0], gate_up.shape[1] // 2
     stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype)
     dh_stride = _matrix("dh", dh, rows, cols, gate_up.dtype)
-    y, fp8, y_stride = _outputs(outputs, out, gate_up, rows, cols, 2)
-    _check(_library().tn_silu_gate_gradients(code, rows, cols, gate_up.data_ptr(), stride, dh.data_ptr(), dh_stride, _ptr(y), y_stride,
-                                             fp8.codes.data_ptr() if fp8 else None, fp8.scales.data_ptr() if fp8 else None, _stream()),
-           "tn_silu_gate_gradients")
+    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, gate_up, rows, cols, 2)
+    _check(_library().tn_silu_gate_gradients(code, rows, cols, gate_up.data_ptr(), stride, dh.data_ptr(), dh_stride, y_ptr, y_stride, codes,
+                                             scales, _stream()), "tn_silu_gate_gradients")
     return RowOutput(y, fp8)
 
 
@@ -374,8 +382,9 @@ class Fp8Linear:
         tensors' outputs lie beside each other."""
         x = self._input(x)
         if out is None:
-            out = torch.empty((x.rows, self.M), dtype=torch.bfloat16, device=self._device)
-        stride = _matrix("out", out, x.rows, self.M, torch.bfloat16)
+            out, stride = torch.empty((x.rows, self.M), dtype=torch.bfloat16, device=self._device), self.M
+        else:
+            stride = _matrix("out", out, x.rows, self.M, torch.bfloat16)
         _check(_lib.tn_fp8_linear_forward(self._handle, x.codes.data_ptr(), x.scales.data_ptr(), out.data_ptr(), stride, x.rows, _stream()),
                "tn_fp8_linear_forward")
         return out
