@@ -17,6 +17,11 @@
 // lets them be read. One barrier a half step.
 // Scale bytes: four K tiles of a row in a word, which the instruction picks its byte from; the words of the next four tiles go to LDS
 // while these four are computed.
+//
+// What bounds it: the matrix cores at the clock that the power limit leaves (busy 78 % of the cycles at 1.75 to 1.9 GHz; where in the loop reads,
+// loads and barriers stand no longer matters). 8192 x 8192 x 8192 in 361 us = 3.04 PFLOP/s, 8192 x 5120 x 25600 in 760 us = 2.82; 256 x 256 tiles take
+// 1.26 us for a K tile, 64 x 256 ones 0.50. Reads with bank conflicts, descriptors in vector registers (every load a
+// loop) and a mask for each load cost 0.4 us of a K tile together.
 // ---------------------------------------------------------------------------------------------
 struct GemmArgs {
     LinearArgs l;
@@ -205,7 +210,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
     __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0): the first half step's loads go where these reads were
     __builtin_amdgcn_s_barrier();
 
-    // The slots of a half step: an MFMA, then what is dealt out there. BAR: all reads of the half step have been issued well before.
+    // The slots of a half step: an MFMA, then what is dealt out there. BAR: where the barrier stands.
     auto half_step = [&](auto idx_c, auto half_c, int kt, unsigned char* s, unsigned char* sn, unsigned char* sc, unsigned char* sc_next) {
         constexpr int IDX = decltype(idx_c)::value, HALF = decltype(half_c)::value;
         constexpr int X = (IDX & 1) ? TH : 0, Y = TH - X;                        // first fragments of x and y
@@ -232,9 +237,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             const intx8 t = __builtin_shufflevector(fa[i][0], fa[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
             acc[i][j] = mfma_block<IDX, IDX>(b, t, acc[i][j], sw[FORM == GEMM_GATED && j >= TH ? 1 : 0], sx[i]);
             __builtin_amdgcn_sched_barrier(0);
-            // reads, one after each MFMA of the quadrant's first ones (all that are left after its last)
-            constexpr int NR = quad ? R1 : R0;
-            constexpr int FROM = m < NR ? m : NR, TO = m == NQ - 1 ? NR : (m + 1 < NR ? m + 1 : NR);
+            // reads, one after each MFMA of the quadrant's first ones, or as many as it takes: all are issued before the barrier, behind which
+            // loads go where they read
+            constexpr int NR = quad ? R1 : R0, SLOTS = quad ? BAR - NQ : NQ, PER = (NR + SLOTS - 1) / SLOTS;
+            static_assert(SLOTS >= 1 && SLOTS * PER >= NR, "reads before the barrier");
+            constexpr int FROM = m * PER < NR ? m * PER : NR, TO = (m + 1) * PER < NR ? (m + 1) * PER : NR;
 #pragma unroll
             for (int n = FROM; n < TO; ++n) {
                 if constexpr (HALF == 0 && quad == 0) read_b(Y + (n >> 1), n & 1, s);
@@ -329,6 +336,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g) {
             m = max(m, unsigned(__shfl_xor(int(m), 32)));
             if (lane_now < 16) top[wn * S::BM + wm * TM * 16 + i * 16 + lane_now] = m;
         }
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0xC07F);          // (no __syncthreads(): it would wait for the next tile's loads)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");

@@ -6,8 +6,8 @@
 // s = x + residual, y = s * r * weight with r = 1 / sqrt(mean(s^2) + eps). Bound by memory: every value is read once and
 // written once, so a row stays in the registers of the waves that read it between the sum of squares and the output: thread t
 // of a workgroup owns its chunks t, t + blockDim.x, ... of 8 elements (NC of them). Rows of a single wave's chunks need no barrier, and
-// a workgroup holds four of them. (8192 rows of 5120, bf16 and residual to bf16 sum, bf16 and 8 bits: 72 us, 5.3 TB/s, which is what a copy
-// reaches.)
+// a workgroup holds four of them. (8192 rows of 5120, bf16 and residual to bf16 sum, bf16 and 8 bits: 69 us, 5.5 TB/s, more than a
+// copy reaches; one row: 3.0 us.)
 // ---------------------------------------------------------------------------------------------
 struct NormArgs {
     const void *x, *residual, *weight;
@@ -90,7 +90,8 @@ __global__ void __launch_bounds__(ONE_WAVE ? 256 : 1024) rms_norm_kernel(NormArg
 // ---------------------------------------------------------------------------------------------
 // dx = r * (g - u * mean(g * u)) + dsum with u = s * r, g = dy * weight; dweight = sum over rows of dy * u. One pass: a
 // workgroup takes every gridDim.x-th row, holds s and dy of a row in registers between its two sums and its output, and adds up
-// dweight for the columns its threads own; its partial sums go to the workspace and norm_grad_reduce_kernel adds them. (8192 rows of 5120 in bf16: 79 us, 4.2 TB/s.)
+// dweight for the columns its threads own; its partial sums go to the workspace and norm_grad_reduce_kernel adds them. (8192 rows of 5120 in bf16: 79 us,
+// 4.2 TB/s; 1024 rows 13 us, 256 workgroups with four rows each, one after another.)
 // ---------------------------------------------------------------------------------------------
 struct NormGradArgs {
     const void *dy, *s, *weight, *dsum;

