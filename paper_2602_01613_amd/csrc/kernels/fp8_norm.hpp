@@ -90,8 +90,12 @@ __global__ void __launch_bounds__(ONE_WAVE ? 256 : 1024) rms_norm_kernel(NormArg
 // ---------------------------------------------------------------------------------------------
 // dx = r * (g - u * mean(g * u)) + dsum with u = s * r, g = dy * weight; dweight = sum over rows of dy * u. One pass: a
 // workgroup takes every gridDim.x-th row, holds s and dy of a row in registers between its two sums and its output, and adds up
-// dweight for the columns its threads own; its partial sums go to the workspace and norm_grad_reduce_kernel adds them. (8192 rows of 5120 in bf16: 79 us,
-// 4.2 TB/s; 1024 rows 13 us, 256 workgroups with four rows each, one after another.)
+// dweight for the columns its threads own; its partial sums go to the workspace and norm_grad_reduce_kernel adds them. (8192 rows of 5120 in bf16:
+// 64 us, 5.2 TB/s; 1024 rows 11.5 us, 256 workgroups with four rows each, one after another.)
+//
+// WHOLE: rows of whole chunks. Their loads have no branches (threads past a row read its last chunk, and what they read counts as zeros; past the
+// last row, that one once more), so that the compiler can wait for a row's loads and leave the next row's under way. With branches it waits
+// for all of them (8192 rows: 84 us).
 // ---------------------------------------------------------------------------------------------
 struct NormGradArgs {
     const void *dy, *s, *weight, *dsum;
@@ -102,7 +106,7 @@ struct NormGradArgs {
     float eps;
 };
 
-template <typename T, int NC>
+template <typename T, int NC, bool WHOLE, bool DSUM>
 __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
     __shared__ float part[2][2][16];
     const int threads = blockDim.x, tid = threadIdx.x, waves = threads >> 6;
@@ -112,32 +116,47 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
     struct Row {
         Chunk<T> s[NC], d[NC], e[NC];
     };
+    auto load = [&](const void* p, int64_t at_row, int c) {
+        const int at = (c * threads + tid) * kChunk;
+        const T* row = static_cast<const T*>(p) + at_row;
+        return WHOLE ? load_chunk(row + min(at, a.cols - kChunk), kChunk) : load_chunk(row + at, a.cols - at);
+    };
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int at = (c * threads + tid) * kChunk;
-        if (weight) w[c] = load_chunk(weight + at, a.cols - at);
+        if (weight) w[c] = load(weight, 0, c);
 #pragma unroll
         for (int i = 0; i < kChunk; ++i) dw[c][i] = 0.f;
     }
-    auto load_row = [&](int64_t row, Row& to) {
+    auto load_row = [&](int row, Row& to) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            const int at = (c * threads + tid) * kChunk, n = a.cols - at;
-            to.s[c] = load_chunk(static_cast<const T*>(a.s) + row * a.s_stride + at, n);
-            to.d[c] = load_chunk(static_cast<const T*>(a.dy) + row * a.dy_stride + at, n);
-            if (a.dsum) to.e[c] = load_chunk(static_cast<const T*>(a.dsum) + row * a.dsum_stride + at, n);
+            to.s[c] = load(a.s, int64_t(row) * a.s_stride, c);
+            to.d[c] = load(a.dy, int64_t(row) * a.dy_stride, c);
+            if (DSUM) to.e[c] = load(a.dsum, int64_t(row) * a.dsum_stride, c);
+        }
+    };
+    auto store = [](auto* p, int n, const float (&v)[kChunk]) {
+        if constexpr (WHOLE) {
+            if (n > 0) store8(p, kChunk, v);
+        } else {
+            store8(p, n, v);
         }
     };
     // (dx may be an input: a row is read whole before it is stored, and only by the workgroup that stores it)
-    auto one_row = [&](int64_t row, const Row& now, int slot) {
+    auto one_row = [&](int row, const Row& now, int slot) {
         float sq = 0.f, dot = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c) {
+            float q = 0.f, g = 0.f;
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) {
-                sq = fmaf(now.s[c][i], now.s[c][i], sq);
-                dot = fmaf(weight ? now.d[c][i] * w[c][i] : now.d[c][i], now.s[c][i], dot);
+                q = fmaf(now.s[c][i], now.s[c][i], q);
+                g = fmaf(weight ? now.d[c][i] * w[c][i] : now.d[c][i], now.s[c][i], g);
             }
+            const bool in = !WHOLE || (c * threads + tid) * kChunk < a.cols;
+            sq += in ? q : 0.f;
+            dot += in ? g : 0.f;
+        }
         sq = wave_sum(sq);
         dot = wave_sum(dot);
         if ((tid & 63) == 0) part[slot][0][tid >> 6] = sq, part[slot][1][tid >> 6] = dot;
@@ -146,7 +165,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
         dot = parts_sum(part[slot][1], waves);
         const float r = 1.f / sqrtf(sq / float(a.cols) + a.eps);
         const float along = dot * r * (r / float(a.cols));          // mean(g * u) * r
-        T* dx = static_cast<T*>(a.dx) + row * a.dx_stride;
+        T* dx = static_cast<T*>(a.dx) + int64_t(row) * a.dx_stride;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             const int at = (c * threads + tid) * kChunk;
@@ -154,26 +173,27 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) {
                 const float u = now.s[c][i] * r;
-                dw[c][i] = fmaf(now.d[c][i], u, dw[c][i]);
+                dw[c][i] = fmaf(now.d[c][i], u, dw[c][i]);           // (past the row: not stored)
                 v[i] = r * (weight ? now.d[c][i] * w[c][i] : now.d[c][i]) - u * along;
-                if (a.dsum) v[i] += now.e[c][i];
+                if (DSUM) v[i] += now.e[c][i];
             }
-            store8(dx + at, a.cols - at, v);
+            store(dx + at, a.cols - at, v);
         }
     };
-    if constexpr (NC == 1) {                         // the next row is under way while this one is summed up
+    const int rows = int(a.rows), step = gridDim.x;  // (at most 2^30 rows)
+    if constexpr (NC == 1 && WHOLE) {                // the next row is under way while this one is summed up
         Row r0, r1;
         load_row(blockIdx.x, r0);                    // the grid has no more workgroups than there are rows
-        for (int64_t row = blockIdx.x; row < a.rows; row += 2 * int64_t(gridDim.x)) {
-            const int64_t second = row + gridDim.x, third = second + gridDim.x;
-            if (second < a.rows) load_row(second, r1);
+        for (int row = blockIdx.x; row < rows; row += 2 * step) {
+            load_row(min(row + step, rows - 1), r1);
             one_row(row, r0, 0);
-            if (third < a.rows) load_row(third, r0);
-            if (second < a.rows) one_row(second, r1, 1);
+            if (row + step >= rows) break;
+            load_row(min(row + 2 * step, rows - 1), r0);
+            one_row(row + step, r1, 1);
         }
-    } else {                                         // no registers for two rows
+    } else {
         int slot = 0;
-        for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, slot ^= 1) {
+        for (int row = blockIdx.x; row < rows; row += step, slot ^= 1) {
             Row r0;
             load_row(row, r0);
             one_row(row, r0, slot);
@@ -184,7 +204,7 @@ __global__ void __launch_bounds__(1024) norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
         const int at = (c * threads + tid) * kChunk;
-        store8(out + at, a.cols - at, dw[c]);
+        store(out + at, a.cols - at, dw[c]);
     }
 }
 
@@ -206,10 +226,7 @@ __global__ void __launch_bounds__(1024) norm_grad_reduce_kernel(const float* par
     }
     part[group][lane] = v;
     __syncthreads();
-    if (group == 0 && col < cols) {
-        float t = 0.f;
-#pragma unroll
-        for (int g = 0; g < 32; ++g) t += part[g][lane];
-        dweight[col] = t;
-    }
+    v = row16_sum(part[lane][group]);                // the other way round: a half wave adds up one column
+    v += __shfl_xor(v, 16);
+    if (lane == 0 && blockIdx.x * 32 + group < cols) dweight[blockIdx.x * 32 + group] = v;
 }

@@ -64,18 +64,26 @@ int dispatch_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
     return chunks <= 1024 ? run_norm<T, 1>(a, chunks, stream) : run_norm<T, 2>(a, chunks, stream);
 }
 
-// Workgroups of the gradient's one pass: what the 256 CUs hold at a time, and no more, since each adds a row of partial sums. (8192 rows of
-// 5120: 79 us with 256 workgroups of 10 waves, 94 with 409; 4096 rows of 1024: 16 us with 1280 of two waves, 25 with 3840.)
+// Workgroups of the gradient's one pass: about ten waves to a CU, and no more, since each adds a row of partial sums. (us with this many, and
+// with twice as many: 8192 rows of 5120 63 + 5 / 66 + 5, 1024 rows 12 + 4 / 14 + 4, 4096 rows of 1024 10 + 5 / 11 + 9.)
 int64_t norm_grad_groups(int64_t rows, int64_t cols) {
     const int64_t waves = div_up(div_up(cols, kChunk), 64), groups = 256 * (waves < 10 ? 10 / waves : 1);
     return rows < groups ? rows : groups;
 }
 
+template <typename T, int NC>
+int run_norm_grad(const NormGradArgs& a, int64_t chunks, int64_t groups, hipStream_t stream) {
+    const dim3 grid{unsigned(groups)}, block{row_threads(chunks, NC)};
+    const bool whole = a.cols % kChunk == 0;
+    if (whole && a.dsum) norm_grad_kernel<T, NC, true, true><<<grid, block, 0, stream>>>(a);
+    else if (whole) norm_grad_kernel<T, NC, true, false><<<grid, block, 0, stream>>>(a);
+    else if (a.dsum) norm_grad_kernel<T, NC, false, true><<<grid, block, 0, stream>>>(a);
+    else norm_grad_kernel<T, NC, false, false><<<grid, block, 0, stream>>>(a);
+    return launched();
+}
 template <typename T>
 int dispatch_norm_grad(const NormGradArgs& a, int64_t chunks, int64_t groups, hipStream_t stream) {
-    if (chunks <= 1024) norm_grad_kernel<T, 1><<<dim3(unsigned(groups)), dim3(row_threads(chunks, 1)), 0, stream>>>(a);
-    else norm_grad_kernel<T, 2><<<dim3(unsigned(groups)), dim3(row_threads(chunks, 2)), 0, stream>>>(a);
-    return launched();
+    return chunks <= 1024 ? run_norm_grad<T, 1>(a, chunks, groups, stream) : run_norm_grad<T, 2>(a, chunks, groups, stream);
 }
 
 template <int OP>
