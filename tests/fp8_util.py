@@ -73,5 +73,6 @@ FORM_CASES = [
     (1, 100, 3000, 600), (1, 2048, 5120, 24), (1, 520, 8192, 80), (1, 520, 25600, 400), (1, 5120, 3000, 100), (1, 520, 25600, 777),
     (0, 1500, 100, 4096), (0, 4100, 256, 4096), (0, 2600, 100, 6000), (0, 25600, 4096, 600), (0, 25600, 256, 777), (0, 4100, 1000, 4096),
     (0, 2600, 512, 8192), (0, 4100, 256, 6000), (0, 2600, 2048, 6000), (0, 10000, 100, 3000),
+    (1, 8192, 1000, 5), (0, 25600, 1000, 6), (0, 5120, 4096, 16),
     (1, 300, 100, 6000), (1, 12000, 1000, 600), (1, 10000, 1000, 777), (1, 2600, 512, 4096), (1, 16000, 256, 777), (1, 5120, 100, 3000),
 ]
