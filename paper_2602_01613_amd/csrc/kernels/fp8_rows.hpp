@@ -12,7 +12,7 @@ struct RowArgs {
     void* y;
     unsigned char *codes, *scales;
     int64_t x_stride, dh_stride, y_stride;
-    int64_t items;             // rows * per_row
+    int64_t items;             // rows of this launch * per_row
     RowLayout out;
     int32_t cols, per_row, segments;
 };

@@ -34,6 +34,14 @@ RowLayout row_layout(int64_t cols, int32_t segments) {
     return l;
 }
 
+// A launch has fewer than 2^32 threads: kernels that give every row threads of their own take longer inputs in runs of rows, of up to
+// this many threads each.
+constexpr int64_t kLaunchThreads = int64_t(1) << 31;
+template <typename P>
+void advance(P*& p, int64_t bytes) {
+    if (p) p = reinterpret_cast<P*>(reinterpret_cast<uintptr_t>(p) + uintptr_t(bytes));
+}
+
 bool sizes_fit(int64_t rows, int64_t cols) { return rows <= kMaxRows && cols <= kMaxCols; }
 // a matrix the caller gives: there, its rows apart, its elements aligned
 bool matrix_ok(const void* p, int64_t stride, int64_t cols, int32_t dtype) { return p && stride >= cols && aligned(p, unsigned(element_bytes(dtype))); }
@@ -54,7 +62,7 @@ int run_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
     return launched();
 }
 template <typename T>
-int dispatch_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
+int norm_rows(const NormArgs& a, int64_t chunks, hipStream_t stream) {
     if (chunks <= 64) {
         rms_norm_kernel<T, 1, true><<<dim3(unsigned(div_up(a.rows, 4))), dim3(256), 0, stream>>>(a);
         return launched();
@@ -62,6 +70,22 @@ int dispatch_norm(const NormArgs& a, int64_t chunks, hipStream_t stream) {
     // one chunk to a thread as far as a workgroup goes: more waves with their loads under way (8192 rows of 5120: 72 us with 10 waves, 93
     // with 5 of two chunks each)
     return chunks <= 1024 ? run_norm<T, 1>(a, chunks, stream) : run_norm<T, 2>(a, chunks, stream);
+}
+template <typename T>
+int dispatch_norm(NormArgs a, int64_t chunks, hipStream_t stream) {
+    constexpr int64_t run = kLaunchThreads / 1024;
+    int rc = TN_OK;
+    for (int64_t left = a.rows; left > 0 && rc == TN_OK; left -= run) {
+        a.rows = left < run ? left : run;
+        rc = norm_rows<T>(a, chunks, stream);
+        advance(a.x, run * a.x_stride * int64_t(sizeof(T)));
+        advance(a.residual, run * a.residual_stride * int64_t(sizeof(T)));
+        advance(a.sum, run * a.sum_stride * int64_t(sizeof(T)));
+        advance(a.y, run * a.y_stride * int64_t(sizeof(T)));
+        advance(a.codes, run * a.out.code_stride);
+        advance(a.scales, run * a.out.scale_stride);
+    }
+    return rc;
 }
 
 // Workgroups of the gradient's one pass: about ten waves to a CU, and no more, since each adds a row of partial sums. (us with this many, and
@@ -87,13 +111,22 @@ int dispatch_norm_grad(const NormGradArgs& a, int64_t chunks, int64_t groups, hi
 }
 
 template <int OP>
-int run_rows(int32_t dtype, int64_t rows, const RowArgs& a, hipStream_t stream) {
-    if (rows == 0) return TN_OK;
-    const int64_t groups = div_up(a.items, 256);
-    if (groups > INT32_MAX) return TN_ERR_UNSUPPORTED;
-    if (dtype == TN_DTYPE_F32) row_kernel<float, OP><<<dim3(unsigned(groups)), dim3(256), 0, stream>>>(a);
-    else row_kernel<bf16_t, OP><<<dim3(unsigned(groups)), dim3(256), 0, stream>>>(a);
-    return launched();
+int run_rows(int32_t dtype, int64_t rows, RowArgs a, hipStream_t stream) {
+    const int64_t run = kLaunchThreads / a.per_row, size = element_bytes(dtype);      // (per_row is 2^29 at the most)
+    int rc = TN_OK;
+    for (int64_t left = rows; left > 0 && rc == TN_OK; left -= run) {
+        a.items = (left < run ? left : run) * a.per_row;
+        const dim3 grid(unsigned(div_up(a.items, 256)));
+        if (dtype == TN_DTYPE_F32) row_kernel<float, OP><<<grid, dim3(256), 0, stream>>>(a);
+        else row_kernel<bf16_t, OP><<<grid, dim3(256), 0, stream>>>(a);
+        rc = launched();
+        advance(a.x, run * a.x_stride * size);
+        advance(a.dh, run * a.dh_stride * size);
+        advance(a.y, run * a.y_stride * size);
+        advance(a.codes, run * a.out.code_stride);
+        advance(a.scales, run * a.out.scale_stride);
+    }
+    return rc;
 }
 
 }  // namespace
@@ -364,7 +397,6 @@ int tn_fp8_quantize(int32_t dtype, int64_t rows, int64_t cols, int32_t segments,
     a.cols = int32_t(cols);
     a.segments = segments;
     a.per_row = int32_t(a.out.code_stride / kChunk);
-    a.items = rows * a.per_row;
     return run_rows<ROW_QUANTIZE>(dtype, rows, a, static_cast<hipStream_t>(stream));
 }
 
@@ -460,7 +492,6 @@ int tn_silu_gate(int32_t dtype, int64_t rows, int64_t cols, const void* gate_up,
     a.cols = int32_t(cols);
     a.segments = 1;
     a.per_row = a.out.blocks * (kBlock / kChunk);
-    a.items = rows * a.per_row;
     return run_rows<ROW_GATE>(dtype, rows, a, static_cast<hipStream_t>(stream));
 }
 
@@ -486,7 +517,6 @@ int tn_silu_gate_gradients(int32_t dtype, int64_t rows, int64_t cols, const void
     a.cols = int32_t(cols);
     a.segments = 2;
     a.per_row = a.out.blocks * (kBlock / kChunk);
-    a.items = rows * a.per_row;
     return run_rows<ROW_GATE_GRAD>(dtype, rows, a, static_cast<hipStream_t>(stream));
 }
 

@@ -156,6 +156,8 @@ class Fp8Rows:
         new = cls.__new__(cls)
         new.codes = torch.empty((rows, blocks * TN_FP8_BLOCK), dtype=_CODES, device=device)
         new.scales = torch.empty((rows, -(-blocks // 4) * 4), dtype=_SCALES, device=device)
+        if not new.codes.is_cuda:
+            raise ValueError("Fp8Rows live on a GPU")
         new.rows, new.cols, new.segments, new._parts = rows, cols, segments, None
         return new
 

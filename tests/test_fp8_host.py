@@ -195,6 +195,11 @@ def test_binding_refuses_host_tensors():
             tn.Fp8Linear([x], 1)
 
 
+def test_rows_in_host_memory_cannot_be_made():
+    with pytest.raises(ValueError):
+        tn.Fp8Rows.empty(2, 200, device="cpu")
+
+
 TILES = [(64, 256), (96, 256), (128, 256), (160, 256), (192, 256), (224, 256), (256, 256), (64, 128), (96, 128), (128, 128), (192, 128), (256, 128)]
 
 

@@ -231,6 +231,40 @@ def test_offsets_past_32_bits():
     assert torch.equal(h[-4:], tn.silu_gate(last, "y").y)
 
 
+def test_more_rows_than_one_launch_takes():
+    """2^32 threads and more in a launch are refused by the runtime, so long inputs go in runs of rows. Rows repeat here with a prime period:
+    each has the bits that a short call gives it."""
+    period = 4099
+
+    def repeats(small, rows, make):
+        x = small.repeat(-(-rows // period), 1)[:rows]
+        got, want = make(x), make(small)
+        del x
+        for g, w in zip(got, want):
+            g, w = g.view(torch.uint8), w.view(torch.uint8)
+            whole = rows // period * period
+            assert g.shape[0] == rows and torch.equal(g[whole:], w[:rows - whole])
+            g = g[:whole].view(-1, *w.shape)
+            for at in range(0, g.shape[0], 4096):
+                assert bool((g[at:at + 4096] == w).all())
+
+    def norm(x):
+        n = tn.rms_norm(x, None, EPS, residual=x, outputs="both")
+        return n.y, n.sum, n.fp8.codes, n.fp8.scales
+
+    def quantised(x):
+        q = tn.quantize_fp8(x)
+        return q.codes, q.scales
+
+    small = dev(rng_of(10).standard_normal((period, 8)))
+    repeats(small, (1 << 21) + 5, norm)                                            # the norm's runs have 2^21 rows
+    repeats(small, (1 << 26) + 5, lambda x: (tn.rms_norm(x, None, EPS).y,))        # a wave to a row: 2^32 threads
+    rows = (1 << 28) + 5                                                            # 16 lanes to a row: 2^32 threads
+    repeats(small[:, :2].contiguous(), rows, lambda x: (tn.silu_gate(x, "y").y,))
+    repeats(small[:, :2].contiguous(), rows, lambda x: (tn.silu_gate_gradients(x, x[:, 1:], "y").y,))
+    repeats(small[:, :1].contiguous(), (1 << 27) + 5, quantised)                   # two runs, with codes
+
+
 def test_on_a_stream_of_its_own_and_in_a_graph():
     rng = rng_of(9)
     x, res, w = dev(activations(rng, 33, 1500)), dev(activations(rng, 33, 1500)), dev(np.ones(1500))
