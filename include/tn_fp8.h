@@ -25,6 +25,7 @@
  * launches, so that they can be captured into a graph. rows == 0 is a no-op where nothing is left to compute. No function
  * throws; all return TN_OK or an error of tn_linear.h, and nothing is launched after an error in the arguments. Results are
  * the same from call to call, bit for bit, for the same inputs and sizes.
+ * Rows (tokens): up to 2^30; columns: up to 2^24 where no other limit is given. More is TN_ERR_UNSUPPORTED.
  */
 #ifndef TN_FP8_H
 #define TN_FP8_H
