@@ -42,15 +42,16 @@ __device__ __forceinline__ unsigned codes4(float a, float b, float c, float d, f
     return finite_codes4(nan_unless_finite(a), nan_unless_finite(b), nan_unless_finite(c), nan_unless_finite(d), inv);
 }
 
-// 1 / (1 + exp(-v)) to 4 units of fp32's last place, in 8 instructions where expf and a division take 30: the exponent v * log2(e) in two parts,
-// of which the hardware's 2^x takes the first. Past +-100 the result does not change (0 and 1); a NaN comes out as something finite, and
-// makes a NaN where it is multiplied with v itself.
+// 1 / (1 + exp(-v)) to 4 units of fp32's last place (below 2^-126: 0), in 8 instructions where expf and a division take 30: the exponent
+// v * log2(e) in two parts, of which the hardware's 2^x takes the first. The second is a residue of either sign, applied as the positive factor
+// 1 + rest * ln(2): below v = -88.72 the power is infinite, and so is its product with the factor, which makes the result 0. Past +-100 the
+// result does not change (1 and 0). A NaN comes out as something finite, and makes a NaN where it is multiplied with v itself.
 __device__ __forceinline__ float sigmoid(float v) {
     const float c = __builtin_amdgcn_fmed3f(v, -100.f, 100.f);
     const float t = c * -1.44269504f;
     const float rest = fmaf(c, -1.44269504f, -t) + c * -1.92596299e-8f;
-    const float e = __builtin_amdgcn_exp2f(t);
-    return __builtin_amdgcn_rcpf(1.f + fmaf(e, rest * 0.693147181f, e));
+    const float factor = fmaf(rest, 0.693147181f, 1.f);
+    return __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), factor, 1.f));
 }
 
 // Maximum over a row of 16 lanes, left in all of them: rotations by 8, 4, 2 and 1 within the row.

@@ -177,6 +177,42 @@ def test_silu_gate_at_the_ends():
     assert g[0] == 1.0 and abs(g[1]) < 1e-30 and g[2] == 2.0 and g[4] == 0 and np.isnan(g[8])
 
 
+def gates_everywhere(dtype):
+    """Every bf16 value within +-128 and, in fp32, dense runs of values where exp(-gate) leaves fp32's range and between: [rows, 1000]."""
+    bits = torch.arange(0x4300 + 1, dtype=torch.int32)                         # 0 .. 128
+    v = (bits << 16).view(torch.float32).double().numpy()
+    v = np.concatenate([v, -v])
+    if dtype == "f32":
+        v = np.concatenate([v, np.linspace(-105, -80, 20001), np.linspace(80, 105, 4001), np.linspace(-128, 128, 8001)])
+    return np.resize(rounded(v, dtype), (-(-v.size // 1000), 1000))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_silu_gate_and_gradients_of_every_gate(dtype):
+    """Finite for finite gates, and within what fp32 and one rounding take off: 2^-20 of each term as above, and 1 / (1 + exp(-gate)) itself to
+    2^-126, the least that a reciprocal that drops subnormal results has to be off by."""
+    gate = gates_everywhere(dtype)
+    rng = rng_of(12)
+    up, dh = (rounded(v, dtype) for v in (rng.standard_normal(gate.shape), rng.standard_normal(gate.shape)))
+    both = np.concatenate([gate, up], axis=1)
+    got, grads = tn.silu_gate(dev(both, dtype), "both"), tn.silu_gate_gradients(dev(both, dtype), dev(dh, dtype), "both")
+    with np.errstate(over="ignore"):
+        sig = 1 / (1 + np.exp(-gate))
+    off = 2.0 ** -20 * sig + 2.0 ** -126
+    slack = 2.0 ** -126                                                        # of a result so small itself
+    ref, (dg, du) = Q.silu_gate(gate, up), Q.silu_gate_gradients(gate, up, dh)
+    close(host(got.y), ref, dtype, off * np.abs(gate * up) + slack)
+    close(host(grads.y[:, :1000]), dg, dtype, off * np.abs(dh * up) * (1 + np.abs(gate)) + slack)
+    close(host(grads.y[:, 1000:]), du, dtype, off * np.abs(dh * gate) + slack)
+    # 8 bits: of the values in fp32, bit for bit, whatever the inputs' type
+    wide, wide_grads = tn.silu_gate(dev(both, "f32"), "both"), tn.silu_gate_gradients(dev(both, "f32"), dev(dh, "f32"), "both")
+    for rows8, twin, segment, values in ((got.fp8, wide.fp8, 0, wide.y), (grads.fp8, wide_grads.fp8, 0, wide_grads.y[:, :1000]),
+                                         (grads.fp8, wide_grads.fp8, 1, wide_grads.y[:, 1000:])):
+        codes, exps = Q.quantize(host(values))
+        for r in (rows8, twin):
+            assert np.array_equal(host(r.values(segment)), codes) and np.array_equal(exponents(r.block_scales(segment)), exps)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,cols,segments", [(1, 1, 1), (3, 127, 1), (2, 128, 2), (5, 129, 2), (4, 1001, 3), (70, 640, 1), (2, 25600, 2)])
 def test_quantize(rows, cols, segments, dtype):
