@@ -1,7 +1,8 @@
 """ctypes binding of the operators around 8-bit projections (include/tn_fp8.h): argument marshalling only.
 
 Root-mean-square norm with the residual's addition, silu(gate) * up, products of 8-bit weights with 8-bit activations, and
-the gradients of all three. Tensors are torch CUDA (ROCm) tensors; work goes to the current HIP stream. Nothing here computes.
+the gradients of all three. Tensors are torch CUDA (ROCm) tensors on the current GPU; work goes to its current HIP stream. Nothing
+here computes.
 
     layer = tn.Fp8Linear([w_gate, w_up], max_tokens=8192)        # bf16 or fp32 [M, N] weights, quantised at create
     n = tn.rms_norm(x, weight, residual=res, outputs="fp8")      # n.sum = x + res, n.fp8 = the norm in 8 bits
@@ -97,19 +98,28 @@ def _check(status: int, where: str) -> None:
 
 # The binding's own time is most of a small call's. torch.cuda.current_stream() builds an object (2.8 us); this is what it asks (0.1).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _stream() -> int:
-    """The current HIP stream of the current device."""
+def _stream(gpu: int) -> int:
+    """The current HIP stream of that GPU."""
     if _raw_stream is None:
-        return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch._C._cuda_getDevice())
+        return torch.cuda.current_stream(gpu).cuda_stream
+    return _raw_stream(gpu)
 
 
-def _matrix(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype) -> int:
-    """The row stride of t, a CUDA [rows, cols] matrix of dtype whose rows are contiguous and apart."""
-    if not (t.dtype is dtype and t.shape == (rows, cols) and t.is_cuda):
-        raise ValueError(f"{name} must be a CUDA [{rows}, {cols}] tensor of {dtype}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+# Launches go to the current GPU, and nothing maps another one's memory there: every tensor of a call must be on it. (get_device() of a tensor
+# in host memory is -1.)
+def _here(name: str, gpu: int) -> int:
+    if gpu != _current_gpu():
+        raise ValueError(f"{name} is on GPU {gpu}, and GPU {_current_gpu()} is the current one")
+    return gpu
+
+
+def _matrix(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, gpu: int) -> int:
+    """The row stride of t, a [rows, cols] matrix of dtype on that GPU whose rows are contiguous and apart."""
+    if not (t.dtype is dtype and t.shape == (rows, cols) and t.get_device() == gpu):
+        raise ValueError(f"{name} must be a [{rows}, {cols}] tensor of {dtype} on GPU {gpu}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
     stride, step = t.stride()
     if rows <= 1:
         stride = cols
@@ -118,19 +128,19 @@ def _matrix(name: str, t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype
     return stride
 
 
-def _input(name: str, t: torch.Tensor) -> int:
-    """The type code of an input matrix that sets the type of a call."""
+def _input(name: str, t: torch.Tensor) -> Tuple[int, int]:
+    """(type code, GPU) of an input matrix that sets the type of a call: on the current GPU."""
     code = _DTYPE.get(t.dtype)
     if code is None or t.dim() != 2 or t.shape[1] < 1 or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA [rows, cols] tensor of float32 or bfloat16, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-    return code
+    return code, _here(name, t.get_device())
 
 
-def _vector(name: str, t: Optional[torch.Tensor], cols: int, dtype: torch.dtype) -> Optional[int]:
+def _vector(name: str, t: Optional[torch.Tensor], cols: int, dtype: torch.dtype, gpu: int) -> Optional[int]:
     if t is None:
         return None
-    if not (t.is_cuda and t.dtype == dtype and t.dim() == 1 and t.shape[0] == cols and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous CUDA [{cols}] tensor of {dtype}")
+    if not (t.get_device() == gpu and t.dtype == dtype and t.dim() == 1 and t.shape[0] == cols and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous [{cols}] tensor of {dtype} on GPU {gpu}")
     return t.data_ptr()
 
 
@@ -146,8 +156,9 @@ class Fp8Rows:
         rows = codes.shape[0]
         if not (codes.is_cuda and codes.dtype == _CODES and codes.is_contiguous() and tuple(codes.shape) == (rows, width)):
             raise ValueError(f"codes must be a contiguous CUDA [rows, {width}] tensor of float8_e4m3fn")
-        if not (scales.is_cuda and scales.dtype == _SCALES and scales.is_contiguous() and tuple(scales.shape) == (rows, -(-blocks // 4) * 4)):
-            raise ValueError(f"scales must be a contiguous CUDA [{rows}, {-(-blocks // 4) * 4}] tensor of float8_e8m0fnu")
+        if not (scales.get_device() == codes.get_device() and scales.dtype == _SCALES and scales.is_contiguous()
+                and tuple(scales.shape) == (rows, -(-blocks // 4) * 4)):
+            raise ValueError(f"scales must be a contiguous [{rows}, {-(-blocks // 4) * 4}] tensor of float8_e8m0fnu on the GPU of codes")
         self.codes, self.scales, self.rows, self.cols, self.segments, self._parts = codes, scales, rows, cols, segments, None
 
     @classmethod
@@ -182,9 +193,11 @@ class Fp8Rows:
     def block_scales(self, segment: int = 0) -> torch.Tensor:
         return self._segment(segment)[1]
 
-    def _ready(self, name: str, rows: int, cols: int, segments: int) -> "Fp8Rows":
+    def _ready(self, name: str, rows: int, cols: int, segments: int, gpu: int) -> "Fp8Rows":
         if (self.rows, self.cols, self.segments) != (rows, cols, segments):
             raise ValueError(f"{name} holds [{self.rows}, {self.segments} x {self.cols}], not [{rows}, {segments} x {cols}]")
+        if self.codes.get_device() != gpu:
+            raise ValueError(f"{name} is on {self.codes.device}, not on GPU {gpu}")
         return self
 
 
@@ -198,7 +211,7 @@ class RowOutput(NamedTuple):
 _OUTPUTS = {"y": (True, False), "fp8": (False, True), "both": (True, True)}
 
 
-def _outputs(outputs: str, out: Optional[RowOutput], like: torch.Tensor, rows: int, cols: int, segments: int):
+def _outputs(outputs: str, out: Optional[RowOutput], like: torch.Tensor, rows: int, cols: int, segments: int, gpu: int):
     """(y, its address, its row stride, fp8, the addresses of its codes and scales) of a call: the caller's, or new ones."""
     want = _OUTPUTS.get(outputs)
     if want is None:
@@ -207,13 +220,16 @@ def _outputs(outputs: str, out: Optional[RowOutput], like: torch.Tensor, rows: i
     if want[0]:
         if out is not None and out.y is not None:
             y = out.y
-            stride = _matrix("out.y", y, rows, segments * cols, like.dtype)
+            stride = _matrix("out.y", y, rows, segments * cols, like.dtype, gpu)
         else:
             stride = segments * cols
             y = like.new_empty((rows, stride))
         y_ptr = y.data_ptr()
     if want[1]:
-        fp8 = out.fp8._ready("out.fp8", rows, cols, segments) if out is not None and out.fp8 is not None else Fp8Rows.empty(rows, cols, segments, like.device)
+        if out is not None and out.fp8 is not None:
+            fp8 = out.fp8._ready("out.fp8", rows, cols, segments, gpu)
+        else:
+            fp8 = Fp8Rows.empty(rows, cols, segments, like.device)
         codes, scales = fp8.codes.data_ptr(), fp8.scales.data_ptr()
     return y, y_ptr, stride, fp8, codes, scales
 
@@ -224,14 +240,14 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def quantize_fp8(x: torch.Tensor, segments: int = 1, out: Optional[Fp8Rows] = None) -> Fp8Rows:
     """x [rows, segments * cols] in 8 bits, each segment in blocks of its own."""
-    code = _input("x", x)
+    code, gpu = _input("x", x)
     rows, width = x.shape
     if segments < 1 or width % segments:
         raise ValueError(f"x has {width} columns: not {segments} equal segments")
     cols = width // segments
-    stride = _matrix("x", x, rows, width, x.dtype)
-    out = Fp8Rows.empty(rows, cols, segments, x.device) if out is None else out._ready("out", rows, cols, segments)
-    _check(_library().tn_fp8_quantize(code, rows, cols, segments, x.data_ptr(), stride, out.codes.data_ptr(), out.scales.data_ptr(), _stream()),
+    stride = _matrix("x", x, rows, width, x.dtype, gpu)
+    out = Fp8Rows.empty(rows, cols, segments, x.device) if out is None else out._ready("out", rows, cols, segments, gpu)
+    _check(_library().tn_fp8_quantize(code, rows, cols, segments, x.data_ptr(), stride, out.codes.data_ptr(), out.scales.data_ptr(), _stream(gpu)),
            "tn_fp8_quantize")
     return out
 
@@ -241,21 +257,21 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float 
     """s = x + residual (in x's type), y = s / sqrt(mean(s^2) + eps) * weight. `outputs`: "y" (x's type), "fp8" (8 bits) or
     "both". Returns (y, fp8, sum); sum is s where there is a residual, and may be given as out.sum (x and residual
     themselves too)."""
-    code = _input("x", x)
+    code, gpu = _input("x", x)
     rows, cols = x.shape
-    x_stride = _matrix("x", x, rows, cols, x.dtype)
-    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, x, rows, cols, 1)
+    x_stride, weight_ptr = _matrix("x", x, rows, cols, x.dtype, gpu), _vector("weight", weight, cols, x.dtype, gpu)
+    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, x, rows, cols, 1, gpu)
     total, total_ptr, res_ptr, res_stride, sum_stride = None, None, None, 0, 0
     if residual is not None:
-        res_stride, res_ptr = _matrix("residual", residual, rows, cols, x.dtype), residual.data_ptr()
+        res_stride, res_ptr = _matrix("residual", residual, rows, cols, x.dtype, gpu), residual.data_ptr()
         if out is not None and out.sum is not None:
             total = out.sum
-            sum_stride = _matrix("out.sum", total, rows, cols, x.dtype)
+            sum_stride = _matrix("out.sum", total, rows, cols, x.dtype, gpu)
         else:
             total, sum_stride = x.new_empty((rows, cols)), cols
         total_ptr = total.data_ptr()
-    _check(_library().tn_rms_norm(code, rows, cols, x.data_ptr(), x_stride, res_ptr, res_stride, _vector("weight", weight, cols, x.dtype), eps,
-                                  total_ptr, sum_stride, y_ptr, y_stride, codes, scales, _stream()), "tn_rms_norm")
+    _check(_library().tn_rms_norm(code, rows, cols, x.data_ptr(), x_stride, res_ptr, res_stride, weight_ptr, eps, total_ptr, sum_stride, y_ptr,
+                                  y_stride, codes, scales, _stream(gpu)), "tn_rms_norm")
     return RowOutput(y, fp8, total)
 
 
@@ -265,15 +281,15 @@ def rms_norm_gradients(dy: torch.Tensor, s: torch.Tensor, weight: Optional[torch
     """(dx, dweight) of rms_norm for the gradient dy of its y and, where s is read elsewhere too, the gradient dsum that arrives
     there: dx in s's type, for x and the residual alike; dweight in fp32 (None without a weight, or with dweight=False).
     s is what rms_norm returned as sum (x, if it had no residual)."""
-    code = _input("s", s)
+    code, gpu = _input("s", s)
     rows, cols = s.shape
-    s_stride = _matrix("s", s, rows, cols, s.dtype)
-    dy_stride = _matrix("dy", dy, rows, cols, s.dtype)
-    ds_stride = 0 if dsum is None else _matrix("dsum", dsum, rows, cols, s.dtype)
+    s_stride, weight_ptr = _matrix("s", s, rows, cols, s.dtype, gpu), _vector("weight", weight, cols, s.dtype, gpu)
+    dy_stride = _matrix("dy", dy, rows, cols, s.dtype, gpu)
+    ds_stride = 0 if dsum is None else _matrix("dsum", dsum, rows, cols, s.dtype, gpu)
     if dx is None:
         dx, dx_stride = s.new_empty((rows, cols)), cols
     else:
-        dx_stride = _matrix("dx", dx, rows, cols, s.dtype)
+        dx_stride = _matrix("dx", dx, rows, cols, s.dtype, gpu)
     lib = _library()
     dw, space, need = None, None, 0
     if dweight and weight is not None:
@@ -282,31 +298,30 @@ def rms_norm_gradients(dy: torch.Tensor, s: torch.Tensor, weight: Optional[torch
             _check(int(need), "tn_rms_norm_gradients_workspace")
         dw = s.new_empty((cols,), dtype=torch.float32)
         space = s.new_empty((need,), dtype=torch.uint8)
-    _check(lib.tn_rms_norm_gradients(code, rows, cols, dy.data_ptr(), dy_stride, s.data_ptr(), s_stride, _vector("weight", weight, cols, s.dtype),
-                                     eps, _ptr(dsum), ds_stride, dx.data_ptr(), dx_stride, _ptr(dw), _ptr(space), need, _stream()),
-           "tn_rms_norm_gradients")
+    _check(lib.tn_rms_norm_gradients(code, rows, cols, dy.data_ptr(), dy_stride, s.data_ptr(), s_stride, weight_ptr, eps, _ptr(dsum), ds_stride,
+                                     dx.data_ptr(), dx_stride, _ptr(dw), _ptr(space), need, _stream(gpu)), "tn_rms_norm_gradients")
     return dx, dw
 
 
 def silu_gate(gate_up: torch.Tensor, outputs: str = "y", out: Optional[RowOutput] = None) -> RowOutput:
     """silu(gate) * up of gate_up = [gate | up], [rows, 2 * cols]; outputs as in rms_norm."""
-    code = _input("gate_up", gate_up)
+    code, gpu = _input("gate_up", gate_up)
     rows, cols = gate_up.shape[0], gate_up.shape[1] // 2
-    stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype)
-    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, gate_up, rows, cols, 1)
-    _check(_library().tn_silu_gate(code, rows, cols, gate_up.data_ptr(), stride, y_ptr, y_stride, codes, scales, _stream()), "tn_silu_gate")
+    stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype, gpu)
+    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, gate_up, rows, cols, 1, gpu)
+    _check(_library().tn_silu_gate(code, rows, cols, gate_up.data_ptr(), stride, y_ptr, y_stride, codes, scales, _stream(gpu)), "tn_silu_gate")
     return RowOutput(y, fp8)
 
 
 def silu_gate_gradients(gate_up: torch.Tensor, dh: torch.Tensor, outputs: str = "y", out: Optional[RowOutput] = None) -> RowOutput:
     """[dgate | dup] for the gradient dh of silu(gate) * up; in 8 bits they are two segments."""
-    code = _input("gate_up", gate_up)
+    code, gpu = _input("gate_up", gate_up)
     rows, cols = gate_up.shape[0], gate_up.shape[1] // 2
-    stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype)
-    dh_stride = _matrix("dh", dh, rows, cols, gate_up.dtype)
-    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, gate_up, rows, cols, 2)
+    stride = _matrix("gate_up", gate_up, rows, 2 * cols, gate_up.dtype, gpu)
+    dh_stride = _matrix("dh", dh, rows, cols, gate_up.dtype, gpu)
+    y, y_ptr, y_stride, fp8, codes, scales = _outputs(outputs, out, gate_up, rows, cols, 2, gpu)
     _check(_library().tn_silu_gate_gradients(code, rows, cols, gate_up.data_ptr(), stride, dh.data_ptr(), dh_stride, y_ptr, y_stride, codes,
-                                             scales, _stream()), "tn_silu_gate_gradients")
+                                             scales, _stream(gpu)), "tn_silu_gate_gradients")
     return RowOutput(y, fp8)
 
 
@@ -325,7 +340,8 @@ def fp8_plan_query(out_features: int, in_features: int, n_tensors: int, tokens: 
 
 
 class Fp8Linear:
-    """One 8-bit weight [M, N] living on the current GPU, or two that read the same activations (gate and up).
+    """One 8-bit weight [M, N], or two that read the same activations (gate and up), living on the GPU that is current when it is made
+    and has to be current when it is used.
 
     tensors  one or two contiguous CUDA tensors of float32 or bfloat16, quantised in blocks of 128 x 128; or, with `scales`,
              float8_e4m3fn codes and their float8_e8m0fnu scales [ceil(M / 128), ceil(N / 128)]
@@ -345,6 +361,9 @@ class Fp8Linear:
         code = TN_DTYPE_FP8 if scales is not None else _DTYPE.get(first.dtype)
         if code is None or (scales is not None and first.dtype != _CODES) or not all(t.is_cuda and t.is_contiguous() for t in tensors):
             raise ValueError("tensors must be contiguous CUDA tensors of float32 or bfloat16, or of float8_e4m3fn together with their scales")
+        gpu = _here("tensors", first.get_device())
+        if tensors[-1].get_device() != gpu:
+            raise ValueError("tensors must be on one GPU")
         m, n = first.shape
         desc = _Desc()
         desc.dtype, desc.n_tensors, desc.out_features, desc.in_features = code, len(tensors), m, n
@@ -352,32 +371,36 @@ class Fp8Linear:
         desc.tensors = ptrs
         if scales is not None:
             shape = (-(-m // TN_FP8_BLOCK), -(-n // TN_FP8_BLOCK))
-            if len(scales) != len(tensors) or any(not (s.is_cuda and s.is_contiguous() and s.dtype == _SCALES and tuple(s.shape) == shape) for s in scales):
-                raise ValueError(f"scales: one contiguous CUDA {list(shape)} tensor of float8_e8m0fnu for each tensor")
+            if len(scales) != len(tensors) or any(not (s.get_device() == gpu and s.is_contiguous() and s.dtype == _SCALES and tuple(s.shape) == shape) for s in scales):
+                raise ValueError(f"scales: one contiguous {list(shape)} tensor of float8_e8m0fnu for each tensor, on its GPU")
             scale_ptrs = (ctypes.c_void_p * len(tensors))(*[s.data_ptr() for s in scales])
             desc.scales = scale_ptrs
         self._workspace = workspace          # keep the caller's block alive as long as the handle
         if workspace is not None:
-            if not (workspace.is_cuda and workspace.is_contiguous() and workspace.numel() > 0):
-                raise ValueError("workspace must be a contiguous CUDA tensor")
+            if not (workspace.get_device() == gpu and workspace.is_contiguous() and workspace.numel() > 0):
+                raise ValueError("workspace must be a contiguous tensor on the GPU of the tensors")
             desc.workspace, desc.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        desc.max_tokens, desc.flags, desc.stream = int(max_tokens), TN_FLAG_TRANSPOSE if transpose else 0, _stream()
+        desc.max_tokens, desc.flags, desc.stream = int(max_tokens), TN_FLAG_TRANSPOSE if transpose else 0, _stream(gpu)
         h = ctypes.c_void_p(0)
         _check(_library().tn_fp8_linear_create(ctypes.byref(h), ctypes.byref(desc)), "tn_fp8_linear_create")
         self._handle = int(h.value)
         self.shape, self.n_tensors, self.transpose = (m, n), len(tensors), bool(transpose)
-        self._device = first.device
+        self._device, self._gpu = first.device, gpu
         self.M, self.N = self.query(TN_QUERY_OUT_FEATURES), self.query(TN_QUERY_IN_FEATURES)
         self._segments = len(tensors) if transpose else 1
 
-    def _input(self, x) -> Fp8Rows:
+    def _open(self) -> None:
         if self._handle is None:
             raise RuntimeError("layer was closed")
+        _here("the layer", self._gpu)
+
+    def _input(self, x) -> Fp8Rows:
+        self._open()
         if not isinstance(x, Fp8Rows):
             if x.dim() != 2 or x.shape[1] != self.N:
                 raise ValueError(f"x must be [tokens, {self.N}]")
             x = quantize_fp8(x, self._segments)
-        return x._ready("x", x.rows, self.N // self._segments, self._segments)
+        return x._ready("x", x.rows, self.N // self._segments, self._segments, self._gpu)
 
     def forward(self, x, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """bf16 [tokens, M] for x in 8 bits (Fp8Rows), or a float32 / bfloat16 tensor, which is quantised first; two
@@ -386,8 +409,8 @@ class Fp8Linear:
         if out is None:
             out, stride = torch.empty((x.rows, self.M), dtype=torch.bfloat16, device=self._device), self.M
         else:
-            stride = _matrix("out", out, x.rows, self.M, torch.bfloat16)
-        _check(_lib.tn_fp8_linear_forward(self._handle, x.codes.data_ptr(), x.scales.data_ptr(), out.data_ptr(), stride, x.rows, _stream()),
+            stride = _matrix("out", out, x.rows, self.M, torch.bfloat16, self._gpu)
+        _check(_lib.tn_fp8_linear_forward(self._handle, x.codes.data_ptr(), x.scales.data_ptr(), out.data_ptr(), stride, x.rows, _stream(self._gpu)),
                "tn_fp8_linear_forward")
         return out
 
@@ -399,19 +422,18 @@ class Fp8Linear:
             raise ValueError("gated needs a layer of two tensors that is not transposed")
         x = self._input(x)
         m = self.shape[0]
-        out = Fp8Rows.empty(x.rows, m, 1, self._device) if out is None else out._ready("out", x.rows, m, 1)
+        out = Fp8Rows.empty(x.rows, m, 1, self._device) if out is None else out._ready("out", x.rows, m, 1, self._gpu)
         _check(_lib.tn_fp8_linear_gated(self._handle, x.codes.data_ptr(), x.scales.data_ptr(), out.codes.data_ptr(), out.scales.data_ptr(),
-                                        x.rows, _stream()), "tn_fp8_linear_gated")
+                                        x.rows, _stream(self._gpu)), "tn_fp8_linear_gated")
         return out
 
     def quantized_tensor(self, slot: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
         """(codes [M, N], scales [ceil(M / 128), ceil(N / 128)]) of tensor `slot`."""
-        if self._handle is None:
-            raise RuntimeError("layer was closed")
+        self._open()
         m, n = self.shape
         codes = torch.empty((m, n), dtype=_CODES, device=self._device)
         scales = torch.empty((-(-m // TN_FP8_BLOCK), -(-n // TN_FP8_BLOCK)), dtype=_SCALES, device=self._device)
-        _check(_lib.tn_fp8_linear_tensor(self._handle, int(slot), codes.data_ptr(), scales.data_ptr(), _stream()), "tn_fp8_linear_tensor")
+        _check(_lib.tn_fp8_linear_tensor(self._handle, int(slot), codes.data_ptr(), scales.data_ptr(), _stream(self._gpu)), "tn_fp8_linear_tensor")
         return codes, scales
 
     def query(self, what: int) -> int:

@@ -27,6 +27,21 @@ def rounded(a, dtype="bf16"):
     return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(TORCH[dtype]).to(torch.float64).numpy()
 
 
+class OnGpu(torch.Tensor):
+    """A tensor that says that it is on GPU `gpu`, wherever its memory is: for the checks of arguments."""
+    gpu = 0
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return self.gpu
+
+
+def on_gpu(t, gpu):
+    t = t.as_subclass(OnGpu)
+    t.gpu = gpu
+    return t
+
+
 def exponents(scales):
     return scales.contiguous().view(torch.uint8).cpu().numpy().astype(np.int64) - 127
 

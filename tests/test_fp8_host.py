@@ -200,6 +200,28 @@ def test_rows_in_host_memory_cannot_be_made():
         tn.Fp8Rows.empty(2, 200, device="cpu")
 
 
+def test_binding_refuses_tensors_of_another_gpu(monkeypatch):
+    """Kernels go to the current GPU's stream: a tensor elsewhere, or a current GPU that is not the tensors', is refused before any launch."""
+    from fp8_util import on_gpu
+    monkeypatch.setattr(fp8, "_current_gpu", lambda: 0)
+    monkeypatch.setattr(fp8, "_library", lambda: pytest.fail("reached the library"))
+    made = [[on_gpu(torch.empty(shape, dtype=torch.bfloat16), i) for shape in ((4, 256), (256,), (4, 512))] for i in range(2)]
+    e = [(on_gpu(torch.empty((4, 256), dtype=torch.float8_e4m3fn), i), on_gpu(torch.empty((4, 4), dtype=torch.float8_e8m0fnu), i)) for i in range(2)]
+    (x, w, wide), (far, far_w, far_wide) = made
+    far8 = tn.Fp8Rows(*e[1], 256)
+    calls = [lambda: tn.rms_norm(far, far_w), lambda: tn.rms_norm(x, far_w), lambda: tn.rms_norm(x, w, residual=far),
+             lambda: tn.rms_norm(x, w, out=tn.RowOutput(far, None)), lambda: tn.rms_norm(x, w, outputs="fp8", out=tn.RowOutput(None, far8)),
+             lambda: tn.rms_norm(x, w, residual=x, out=tn.RowOutput(x, None, far)),
+             lambda: tn.rms_norm_gradients(far, far, far_w), lambda: tn.rms_norm_gradients(far, x, w), lambda: tn.rms_norm_gradients(x, x, far_w, dweight=False),
+             lambda: tn.rms_norm_gradients(x, x, w, dsum=far), lambda: tn.rms_norm_gradients(x, x, w, dx=far),
+             lambda: tn.silu_gate(far_wide), lambda: tn.silu_gate(wide, out=tn.RowOutput(far, None)),
+             lambda: tn.silu_gate_gradients(wide, far), lambda: tn.silu_gate_gradients(far_wide, far),
+             lambda: tn.quantize_fp8(far), lambda: tn.quantize_fp8(x, out=far8), lambda: tn.Fp8Rows(e[0][0], e[1][1], 256)]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+
+
 TILES = [(64, 256), (96, 256), (128, 256), (160, 256), (192, 256), (224, 256), (256, 256), (64, 128), (96, 128), (128, 128), (192, 128), (256, 128)]
 
 

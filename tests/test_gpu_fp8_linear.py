@@ -5,7 +5,8 @@ import torch
 
 import oracle.fp8_oracle as Q
 import paper_2602_01613_amd as tn
-from fp8_util import FORM_CASES, check_eight_bit, check_padding, dev, exponents, half_unit, host, rounded
+from fp8_util import FORM_CASES, check_eight_bit, check_padding, dev, exponents, half_unit, host, on_gpu, rounded
+from paper_2602_01613_amd import fp8
 
 pytestmark = pytest.mark.gpu
 
@@ -258,6 +259,31 @@ def test_binding_refuses():
         layer.quantized_tensor(2)
     with pytest.raises(tn.TNLinearError):
         layer.query(999)
+
+
+def test_binding_refuses_another_gpu(monkeypatch):
+    """A layer is used on the GPU that it lives on, with tensors there."""
+    w, x = dev(np.ones((128, 256))), dev(np.ones((2, 256)))
+    elsewhere = lambda shape, dtype: on_gpu(torch.empty(shape, dtype=dtype, device="cuda"), 1)      # noqa: E731
+    far, far_w, far_y = (elsewhere(s, torch.bfloat16) for s in ((2, 256), (128, 256), (2, 256)))
+    far8 = tn.Fp8Rows(elsewhere((2, 256), torch.float8_e4m3fn), elsewhere((2, 4), torch.float8_e8m0fnu), 256)
+    out8 = tn.Fp8Rows(elsewhere((2, 128), torch.float8_e4m3fn), elsewhere((2, 4), torch.float8_e8m0fnu), 128)
+    block = elsewhere((1 << 20,), torch.uint8)
+    far_codes, far_scales = elsewhere((128, 256), torch.float8_e4m3fn), elsewhere((1, 2), torch.float8_e8m0fnu)
+    layer = tn.Fp8Linear([w, w], 4)
+    codes, scales = layer.quantized_tensor(0)
+    for call in (lambda: tn.Fp8Linear([far_w], 4), lambda: tn.Fp8Linear([w, far_w], 4), lambda: tn.Fp8Linear([w], 4, workspace=block),
+                 lambda: tn.Fp8Linear([codes], 4, scales=[far_scales]), lambda: tn.Fp8Linear([far_codes], 4, scales=[scales]),
+                 lambda: layer(far), lambda: layer(far8), lambda: layer(x, out=far_y), lambda: layer.gated(far8), lambda: layer.gated(x, out=out8)):
+        with pytest.raises(ValueError):
+            call()
+    rows = tn.quantize_fp8(x)
+    monkeypatch.setattr(fp8, "_current_gpu", lambda: 1)
+    for call in (lambda: layer(rows), lambda: layer.gated(rows), lambda: layer.quantized_tensor(0), lambda: layer(x), lambda: tn.Fp8Linear([w], 4)):
+        with pytest.raises(ValueError):
+            call()
+    monkeypatch.undo()
+    assert torch.equal(layer(rows), layer(x))
 
 
 def exact_rows(codes, scales, rows=1):
