@@ -139,7 +139,7 @@ int tn_fp8_linear_forward(tn_fp8_linear_t h, const void* codes, const void* scal
                           void* stream);
 
 /* silu(X Wg^T) * (X Wu^T) in 8 bits ([tokens, M], one segment), for a handle of two tensors (Wg, Wu) without TN_FLAG_TRANSPOSE:
- * gate and up are not rounded on the way. */
+ * gate and up are not rounded on the way. The output overlaps nothing; on X it is TN_ERR_INVALID_ARG. */
 int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales, void* out_codes, void* out_scales, int64_t tokens,
                         void* stream);
 

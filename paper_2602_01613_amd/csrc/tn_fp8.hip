@@ -48,6 +48,11 @@ bool matrix_ok(const void* p, int64_t stride, int64_t cols, int32_t dtype) { ret
 bool eight_bit_ok(const void* codes, const void* scales) {
     return (!codes && !scales) || (codes && scales && aligned(codes, 16) && aligned(scales, 4));
 }
+// no byte of [p, p + n) in [q, q + m)
+bool apart(const void* p, int64_t n, const void* q, int64_t m) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a + uintptr_t(n) <= b || b + uintptr_t(m) <= a;
+}
 bool float_type(int32_t dtype) { return dtype == TN_DTYPE_F32 || dtype == TN_DTYPE_BF16; }
 
 // ---------------------------------------------------------------------------------------------
@@ -590,6 +595,9 @@ int tn_fp8_linear_gated(tn_fp8_linear_t h, const void* codes, const void* scales
     a.out_code_stride = o.code_stride;
     a.out_scale_stride = o.scale_stride;
     a.spare = o.spare;
+    // workgroups read rows of X while others write theirs of the output
+    if (!apart(codes, tokens * a.code_stride, out_codes, tokens * o.code_stride) || !apart(scales, tokens * a.scale_stride, out_scales, tokens * o.scale_stride))
+        return TN_ERR_INVALID_ARG;
     return run_product(*h, a, true, static_cast<hipStream_t>(stream));
 }
 

@@ -417,7 +417,7 @@ class Fp8Linear:
     __call__ = forward
 
     def gated(self, x, out: Optional[Fp8Rows] = None) -> Fp8Rows:
-        """silu(x Wg^T) * (x Wu^T) in 8 bits, for a layer of two tensors (Wg, Wu)."""
+        """silu(x Wg^T) * (x Wu^T) in 8 bits, for a layer of two tensors (Wg, Wu); not in place of x."""
         if self.n_tensors != 2 or self.transpose:
             raise ValueError("gated needs a layer of two tensors that is not transposed")
         x = self._input(x)

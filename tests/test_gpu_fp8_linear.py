@@ -286,6 +286,21 @@ def test_binding_refuses_another_gpu(monkeypatch):
     assert torch.equal(layer(rows), layer(x))
 
 
+def test_gated_refuses_its_input_as_output():
+    """Square weights: the rows of input and output have one size, and other workgroups still read the input when one writes."""
+    w = dev(np.eye(256))
+    layer, rows = tn.Fp8Linear([w, w], 40), tn.quantize_fp8(dev(np.ones((80, 256))))
+    part = lambda a, b: tn.Fp8Rows(rows.codes[a:b], rows.scales[a:b], 256)      # noqa: E731
+    before = rows.codes.view(torch.uint8).clone()
+    for x, out in ((rows, rows), (part(0, 40), part(39, 79)), (part(20, 60), part(0, 40))):
+        with pytest.raises(tn.TNLinearError):
+            layer.gated(x, out=out)
+    assert torch.equal(rows.codes.view(torch.uint8), before)
+    want = layer.gated(part(0, 40))
+    got = layer.gated(part(0, 40), out=part(40, 80))                  # beside each other is no overlap
+    assert torch.equal(got.codes.view(torch.uint8), want.codes.view(torch.uint8)) and torch.equal(got.scales.view(torch.uint8), want.scales.view(torch.uint8))
+
+
 def exact_rows(codes, scales, rows=1):
     """Codes and scales in 64 bits, on the GPU."""
     n, k = codes.shape
