@@ -54,7 +54,7 @@ int tn_fp8_quantize(int32_t dtype, int64_t rows, int64_t cols, int32_t segments,
  * s = x + residual (added in fp32, rounded to `dtype`; residual NULL: s = x), y = s / sqrt(mean(s^2) + eps) * weight.
  *  weight [cols] of `dtype`, or NULL for ones
  *  sum    NULL, or where s goes; it may be x or residual itself (same stride), but not overlap them otherwise
- *  y      NULL, or y rounded to `dtype`; it may be x itself
+ *  y      NULL, or y rounded to `dtype`; it may be x or residual itself (same stride), but not sum
  *  codes, scales  NULL both, or y in 8 bits, quantised from fp32 (one segment)
  * One of sum, y and codes is needed at the least. The mean and y are computed in fp32 from s as it is rounded, which is what
  * the gradients below are given. cols <= TN_FP8_MAX_NORM_COLS.

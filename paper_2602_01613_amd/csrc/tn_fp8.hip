@@ -414,7 +414,7 @@ int tn_rms_norm(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_
     if (!sum && !y && !codes) return TN_ERR_INVALID_ARG;
     if (!matrix_ok(x, x_stride, cols, dtype) || (residual && !matrix_ok(residual, residual_stride, cols, dtype)) ||
         (sum && !matrix_ok(sum, sum_stride, cols, dtype)) || (y && !matrix_ok(y, y_stride, cols, dtype)) ||
-        !aligned(weight, unsigned(element_bytes(dtype))) || !eight_bit_ok(codes, scales))
+        !aligned(weight, unsigned(element_bytes(dtype))) || !eight_bit_ok(codes, scales) || (sum && sum == y))
         return TN_ERR_INVALID_ARG;
     NormArgs a{};
     a.x = x;

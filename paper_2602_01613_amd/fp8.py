@@ -255,8 +255,8 @@ def quantize_fp8(x: torch.Tensor, segments: int = 1, out: Optional[Fp8Rows] = No
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
              outputs: str = "y", out: Optional[RowOutput] = None) -> RowOutput:
     """s = x + residual (in x's type), y = s / sqrt(mean(s^2) + eps) * weight. `outputs`: "y" (x's type), "fp8" (8 bits) or
-    "both". Returns (y, fp8, sum); sum is s where there is a residual, and may be given as out.sum (x and residual
-    themselves too)."""
+    "both". Returns (y, fp8, sum); sum is s where there is a residual, and may be given as out.sum. out.y and out.sum may be x or
+    residual themselves, but not the same tensor."""
     code, gpu = _input("x", x)
     rows, cols = x.shape
     x_stride, weight_ptr = _matrix("x", x, rows, cols, x.dtype, gpu), _vector("weight", weight, cols, x.dtype, gpu)

@@ -135,6 +135,14 @@ def test_nothing_asked_for_is_refused():
     assert lib.tn_silu_gate_gradients(*{**ROW_CALLS["tn_silu_gate_gradients"][0], "y": None, "codes": None, "scales": None}.values()) == INVALID
 
 
+def test_norm_refuses_one_place_for_two_outputs():
+    lib = fp8._library()
+    good = ROW_CALLS["tn_rms_norm"][0]
+    for where in (A, A + 4096):
+        assert lib.tn_rms_norm(*{**good, "sum": where, "y": where, "residual": A}.values()) == INVALID
+        assert lib.tn_rms_norm(*{**good, "sum": where, "y": where, "codes": None, "scales": None}.values()) == INVALID
+
+
 def test_norm_workspace():
     f = fp8._library().tn_rms_norm_gradients_workspace
     assert f(-1, 5) == INVALID and f(5, 0) == INVALID and f(5, 1 << 30) == UNSUPPORTED and f((1 << 30) + 1, 5) == UNSUPPORTED

@@ -68,6 +68,24 @@ def test_rms_norm_without_weight_strided_and_in_place():
     assert torch.equal(z, y[:, :700])
 
 
+@pytest.mark.parametrize("rows,cols", [(6, 300), (5, 700), (3, 9000)])
+def test_rms_norm_in_place_of_both_inputs(rows, cols):
+    """sum and y where x and residual were, either way round; one tensor for both is refused."""
+    rng = rng_of(rows, cols, 13)
+    x, res, w = (dev(v) for v in (activations(rng, rows, cols), activations(rng, rows, cols), 1 + 0.2 * rng.standard_normal(cols)))
+    ref = tn.rms_norm(x, w, EPS, residual=res, outputs="both")
+    for swap in (False, True):
+        x2, res2 = x.clone(), res.clone()
+        y, total = (res2, x2) if swap else (x2, res2)
+        got = tn.rms_norm(x2, w, EPS, residual=res2, outputs="both", out=tn.RowOutput(y, None, total))
+        assert got.y is y and got.sum is total and torch.equal(y, ref.y) and torch.equal(total, ref.sum)
+        assert torch.equal(got.fp8.codes.view(torch.uint8), ref.fp8.codes.view(torch.uint8))
+    before = x.clone()
+    with pytest.raises(tn.TNLinearError):
+        tn.rms_norm(x, w, EPS, residual=res, out=tn.RowOutput(x, None, x))
+    assert torch.equal(x, before)
+
+
 def test_rms_norm_rows_of_zeros_and_of_what_is_not_finite():
     x = np.zeros((5, 300))
     x[1, 7], x[2, 7], x[3] = np.inf, np.nan, 1e-30
