@@ -7,7 +7,8 @@
 // written once, so a row stays in the registers of the waves that read it between the sum of squares and the output: thread t
 // of a workgroup owns its chunks t, t + blockDim.x, ... of 8 elements (NC of them). Rows of a single wave's chunks need no barrier, and
 // a workgroup holds four of them. (8192 rows of 5120, bf16 and residual to bf16 sum, bf16 and 8 bits: 69 us, 5.5 TB/s, more than a
-// copy reaches; one row: 3.0 us.)
+// copy reaches; in fp32 130 us, 5.5; 8192 rows of 5121 in bf16, which are not aligned to a lane's chunks, 94; one row: 3.0 us. Rows of 128, with 16 of
+// a wave's lanes at work: 524288 of them to bf16 alone 150 us, 1.8 TB/s.)
 // ---------------------------------------------------------------------------------------------
 struct NormArgs {
     const void *x, *residual, *weight;
@@ -91,11 +92,12 @@ __global__ void __launch_bounds__(ONE_WAVE ? 256 : 1024) rms_norm_kernel(NormArg
 // dx = r * (g - u * mean(g * u)) + dsum with u = s * r, g = dy * weight; dweight = sum over rows of dy * u. One pass: a
 // workgroup takes every gridDim.x-th row, holds s and dy of a row in registers between its two sums and its output, and adds up
 // dweight for the columns its threads own; its partial sums go to the workspace and norm_grad_reduce_kernel adds them. (8192 rows of 5120 in bf16:
-// 64 us, 5.2 TB/s; 1024 rows 11.5 us, 256 workgroups with four rows each, one after another.)
+// 64 us, 5.2 TB/s; 4096 rows in fp32 67 with the sums of dweight, 5.0; 1024 rows in bf16 11.0 us, 256 workgroups with four rows each, one after another;
+// 524288 rows of 128 228 us, 1.8 TB/s: 16 of a wave's lanes, and a barrier for each row.)
 //
 // WHOLE: rows of whole chunks. Their loads have no branches (threads past a row read its last chunk, and what they read counts as zeros; past the
 // last row, that one once more), so that the compiler can wait for a row's loads and leave the next row's under way. With branches it waits
-// for all of them (8192 rows: 84 us).
+// for all of them (8192 rows: 84 us), and other widths are read so, a row at a time (8192 rows of 5121: 107 us with the sums of dweight, of 5120: 67).
 // ---------------------------------------------------------------------------------------------
 struct NormGradArgs {
     const void *dy, *s, *weight, *dsum;

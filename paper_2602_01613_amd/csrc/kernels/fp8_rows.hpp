@@ -5,7 +5,8 @@
 // ---------------------------------------------------------------------------------------------
 // Bound by memory: one chunk of 8 elements to a lane, every value read and written once. Lanes count chunks of padded rows
 // (whole blocks, so the 16 lanes of a block are in one row and all there); `per_row` of them to a row. (Gradients of 1024 x 2 x 25600 in bf16:
-// 39 us, 5.4 TB/s; 59 with expf, divisions and a NaN check for every code.)
+// 39 us, 5.4 TB/s; 59 with expf, divisions and a NaN check for every code. silu(gate) * up of as many to 8 bits 27 us, 4.9 TB/s. Quantisation of
+// 8192 x 5120 in bf16 27 us, 4.6 TB/s, of 1001 x 5120 5.6 us: half of that is what a launch of few rows takes, 2.7 to 3.3 us for one.)
 // ---------------------------------------------------------------------------------------------
 struct RowArgs {
     const void *x, *dh;

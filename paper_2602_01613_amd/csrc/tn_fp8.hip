@@ -225,7 +225,10 @@ LinearArgs linear_args(const tn_fp8_linear_s& h, const void* codes, const void* 
 // which kernel a product runs on
 // ---------------------------------------------------------------------------------------------
 // Times in us, fitted to measurements on the MI355X (256 CUs) of products of 5120 to 25600 inputs and 1024 to 25600 outputs,
-// 1 to 8192 tokens. What is chosen by them takes no more than 10 % longer than the best form at most of 120 sizes tried, 25 % at the worst.
+// 1 to 8192 tokens. Of 120 sizes tried (1 to 4096 tokens, outputs and inputs of 700 to 25600) the form chosen by them is within 2 % of the
+// best at 86 and over 10 % longer at 14; 9 of these are 700 to 6000 outputs of up to 5120 inputs at 64 to 257 tokens, streamed with one or two runs
+// of features to a workgroup where more, or tiles, would be better (1.47 times at the worst: 150 tokens 5120 -> 1024, 11.4 us for 7.8). Gated: over
+// 10 % at 1 of 55.
 struct TileCost {
     int tm, tn;
     double k_tile, rest;      // a workgroup's time for a K tile, and for a tile's beginning and end (with two on a CU: both of them)
@@ -263,8 +266,9 @@ Choice choose(const LinearArgs& a, bool gated, int64_t workspace_bytes) {
     Choice best;
     // streamed, 16 tokens at a time: the weight comes from memory once, for every further 16 tokens from the caches, and each workgroup
     // reads its tokens. Pieces to a workgroup: one where there are few; two where one each would leave some CUs two workgroups and
-    // others one (320 pieces of 25600 k, one token: 25.4 us with two to a workgroup, 30 with one); with more than four tokens as many as leave two
-    // workgroups or more to a CU (1600 pieces of 5120 k, 16 tokens: 28 us with four, 33 with one).
+    // others one (320 pieces of 25600 k, one token: 25.4 us with two to a workgroup, 30 with one); with more than four tokens, which a
+    // workgroup reads once for all of its pieces, two up to 1023 pieces and four from 1024 on, where that leaves a workgroup or more to each CU (1600
+    // pieces of 5120 k, 16 tokens: 28 us with four, 33 with one).
     if (a.tokens <= 16 * 65535 && (!gated || outputs <= double(workspace_bytes))) {
         Choice c;
         c.groups = pieces <= kCUs ? 1 : pieces < 2 * kCUs ? 2 : a.tokens <= 4 ? 1 : pieces < 4 * kCUs ? 2 : 4;

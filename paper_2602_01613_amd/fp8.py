@@ -147,7 +147,8 @@ def _vector(name: str, t: Optional[torch.Tensor], cols: int, dtype: torch.dtype,
 class Fp8Rows:
     """Rows in 8 bits: `codes` (float8_e4m3fn [rows, segments * P], P = cols rounded up to 128) and `scales` (float8_e8m0fnu
     [rows, S], one for each block of 128, S rounded up to 4), as include/tn_fp8.h lays them out. `values` and `block_scales`
-    are views of a segment without its padding."""
+    are views of a segment without its padding. Padding has to be zero, codes and scale bytes: every function here writes it so, and
+    products read it. Whoever makes Fp8Rows of codes of their own clears it (a NaN code there makes its row's products NaN)."""
 
     __slots__ = ("codes", "scales", "rows", "cols", "segments", "_parts")
 
