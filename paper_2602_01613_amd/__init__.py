@@ -50,3 +50,16 @@ from .fp8 import (  # noqa: F401
     silu_gate,
     silu_gate_gradients,
 )
+from .int4 import (  # noqa: F401
+    INT4_EXPORTED_SYMBOLS,
+    Int4Linear,
+    TN_DTYPE_F16,
+    TN_DTYPE_INT4,
+    TN_INT4_PLAN_RANGES, TN_INT4_PLAN_STREAM_PIECES, TN_INT4_PLAN_STREAM_TOKENS, TN_INT4_PLAN_TILE_TOKENS,
+    int4_plan_query,
+)
+from .adamw import (  # noqa: F401
+    ADAMW_EXPORTED_SYMBOLS,
+    AdamW,
+    TN_ADAMW_BLOCK,
+)

@@ -30,8 +30,8 @@ def hipcc_path() -> str:
     raise RuntimeError("hipcc not found")
 
 
-# one object each: the factorised layers, and the operators around 8-bit projections
-SOURCES = ("tn_linear.hip", "tn_fp8.hip")
+# one object each: the factorised layers, the operators around 8-bit projections, 4-bit projections, and the AdamW step
+SOURCES = ("tn_linear.hip", "tn_fp8.hip", "tn_int4.hip", "tn_adamw.hip")
 
 
 def _run(cmd, verbose: bool) -> None:

@@ -1,0 +1,276 @@
+// Products of many tokens with 4-bit weights: tokens in LDS, weights made in registers.
+// Part of tn_int4.hip's translation unit, inside its anonymous namespace, after int4_stream.hpp.
+#pragma once
+
+// ---------------------------------------------------------------------------------------------
+// A workgroup of four waves computes 16 * TM tokens x 256 features: each wave all of the tokens x 64 features, in TM x 4 accumulators of
+// v_mfma_f32_16x16x32_bf16. Side by side along the features, no two waves make the same weight: its codes go from memory to registers in the
+// operand's order (1 KB a load) and become bf16 there, 20 vector instructions for 512 weights, dealt out between the MFMAs of the step before.
+// The tokens go from memory to LDS without passing through registers, in three stages of 64 k; a row is 128 bytes there, its 16-byte chunk c at
+// position c ^ ((row / 2) % 8), so that the 16 rows a read touches at a time fall on 16 different slots of the 64 banks.
+//
+// A step is 32 k: 4 * TM MFMAs, tokens outermost. Behind the four of token fragment i the fragment that the next step has in its place is
+// read into the same registers. A stage is two steps; what the first one reads (its second half) are the last reads of the stage, so that after the
+// barrier in the second step the stage after next but one goes where it is.
+// ---------------------------------------------------------------------------------------------
+enum Int4Form : int { INT4_PLAIN = 0, INT4_GATED = 1, INT4_PARTIAL = 2 };
+
+struct Int4GemmArgs {
+    Int4Args l;
+    int32_t n_row, n_col;            // output tiles
+    int32_t band;                    // rows of tiles to a band
+    int32_t blocks_per_split;        // blocks of k to a range
+};
+
+template <int TM>
+struct Int4Shape {
+    static constexpr int BM = 16 * TM, STAGE = BM * 128, NS = 3, SMEM = NS * STAGE;
+    static constexpr int PER_CU = TM <= 8 ? 2 : 1;
+};
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | (0x7 << 4) | (0xF << 8) | ((N >> 4) << 14));
+}
+template <typename F, int... Q>
+__device__ __forceinline__ void for_constants(F&& f, std::integer_sequence<int, Q...>) {
+    (f(std::integral_constant<int, Q>()), ...);
+}
+
+#ifdef __HIP_DEVICE_COMPILE__
+template <int TM, int FORM, bool TRANSPOSED, int SUB>
+__device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
+    using S = Int4Shape<TM>;
+    constexpr int LOADS = TM / 2;                 // of a stage, to a wave: 8 rows each
+    static_assert(TM % 4 == 0, "whole loads for each wave, reads behind the barrier");
+    typedef __attribute__((address_space(3))) void lds_t;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const Int4Args& a = g.l;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // XCD x takes a contiguous eighth of the tiles, in bands of a few rows of them (rows fastest): what runs there at a time shares
+    // panels of both operands in its L2
+    const int n_items = g.n_row * g.n_col * a.n_split, xcd = blockIdx.x & 7;
+    const int item = int(int64_t(n_items) * xcd >> 3) + int(blockIdx.x >> 3);
+    if (item >= int(int64_t(n_items) * (xcd + 1) >> 3)) return;
+    const int tile = item / a.n_split, split = __builtin_amdgcn_readfirstlane(item - tile * a.n_split);
+    const int band = tile / (g.band * g.n_col), in_band = tile - band * (g.band * g.n_col);
+    const int band_rows = min(g.band, g.n_row - band * g.band);
+    const int col_tile = __builtin_amdgcn_readfirstlane(in_band / band_rows);
+    const int row_tile = __builtin_amdgcn_readfirstlane(band * g.band + in_band - col_tile * band_rows);
+    const int kb0 = split * g.blocks_per_split, nk = min(a.k_blocks, kb0 + g.blocks_per_split) - kb0;
+
+    // rows past the last token are out of the buffer's bounds: zeros, no memory is read
+    constexpr int RSRC = 0x00020000;
+    const int row_bytes = int(a.x_stride) * 2, rows = int(min(a.tokens - int64_t(row_tile) * S::BM, int64_t(S::BM)));
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<bf16_t*>(a.x + int64_t(row_tile) * S::BM * a.x_stride), 0, (rows - 1) * row_bytes + a.k_blocks * (kBlock * 2), RSRC);
+    const int vx = (wave * 8 + (lane >> 3)) * row_bytes + (((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))) * 16);
+    const int last_stage = (kb0 + nk) * 2 - 1;
+    auto load_x = [&](int n, int at, unsigned char* s) {              // n: load of the stage; at: stage in memory
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_t*)(s + (wave + 4 * n) * 1024), 16, vx + n * 32 * row_bytes, min(at, last_stage) * 128, 0, 0);
+    };
+
+    // the wave's four pieces: gated, two of gate's and the same two of up's
+    const int all_pieces = a.f_pieces * a.tensors;
+    const int first = FORM == INT4_GATED ? col_tile * 8 + wave * 2 : col_tile * 16 + wave * 4;
+    const bool there = FORM == INT4_GATED ? first < a.f_pieces : first < all_pieces;         // (pieces come in fours)
+    auto piece_of = [&](int f) {
+        const int p = there ? first : 0;
+        return FORM == INT4_GATED ? (f < 2 ? p + f : a.f_pieces + p + f - 2) : p + f;
+    };
+    const unsigned* codes[4];
+    const unsigned* words[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+        codes[f] = a.packed + int64_t(piece_of(f)) * a.k_blocks * kPieceWords + lane * 4;
+        words[f] = TRANSPOSED ? a.words + piece_of(f) / a.group_pieces * a.word_stride + (lane >> 4) * 8
+                              : a.words + int64_t(piece_of(f)) * a.k_blocks * (SUB * kPiece) + (lane & 15);
+    }
+    // Transposed: scales along k, the same for the pieces of a group, of which the wave has SUB (1 for groups of 64 and more, 2 for 32)
+    constexpr int NW = TRANSPOSED ? SUB : 4;
+    struct Words {
+        unsigned w[TRANSPOSED ? 1 : 4][TRANSPOSED ? 1 : SUB];
+    };
+    uintx4 now[4], next[4];
+    Words words_now, words_next;
+    auto load_codes = [&](uintx4 (&to)[4], Words& w, int kb) {
+        const int at = min(kb, kb0 + nk - 1);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) to[f] = *reinterpret_cast<const uintx4*>(codes[f] + int64_t(at) * kPieceWords);
+        if constexpr (!TRANSPOSED) {
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int s = 0; s < SUB; ++s) w.w[f][s] = words[f][(int64_t(at) * SUB + s) * kPiece];
+        }
+    };
+    // transposed: the words of the lane's 8 k of a step
+    uintx4 kw[NW][2];
+    auto load_words = [&](int kb, int j) {
+        const int at = min(kb, kb0 + nk - 1);
+        if constexpr (TRANSPOSED) {
+#pragma unroll
+            for (int n = 0; n < NW; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) kw[n][h] = *reinterpret_cast<const uintx4*>(words[n * (4 / NW)] + int64_t(at) * kBlock + j * 32 + h * 4);
+        }
+    };
+
+    const int r = lane & 15, kq = lane >> 4;
+    const int o0 = r * 128 + ((kq ^ (r >> 1)) * 16), o1 = r * 128 + (((4 + kq) ^ (r >> 1)) * 16);
+    bf16x8 fx[TM];
+    uintx4 fw[2][4];
+    floatx4 acc[TM][4];
+    auto read_x = [&](int i, int half, const unsigned char* s) { fx[i] = *reinterpret_cast<const bf16x8*>(s + (half ? o1 : o0) + i * 2048); };
+    // word `at` of the 16 (pair p of fragment f) of step j
+    auto make = [&](uintx4 (&to)[4], const uintx4 (&c)[4], const Words& w, int j, int at) {
+        const int f = at >> 2, p = at & 3;
+        if constexpr (TRANSPOSED) {
+            const int n = f / (4 / NW);
+            const unsigned w0 = kw[n][p >> 1][2 * (p & 1)], w1 = kw[n][p >> 1][2 * (p & 1) + 1];
+            to[f][p] = weights_as_bf16(c[f][j], p, word_scale(w0), word_offset(w0), word_scale(w1), word_offset(w1));
+        } else {
+            const unsigned s = w.w[f][j * SUB / 4];
+            const float scale = word_scale(s), offset = word_offset(s);
+            to[f][p] = weights_as_bf16(c[f][j], p, scale, offset, scale, offset);
+        }
+    };
+
+    load_codes(now, words_now, kb0);
+    load_words(kb0, 0);
+#pragma unroll
+    for (int q = 0; q < S::NS; ++q)
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) load_x(n, kb0 * 2 + q, smem + q * S::STAGE);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[i][f] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int at = 0; at < 16; ++at) make(fw[0], now, words_now, 0, at);
+    load_words(kb0, 1);
+    wait_vmcnt<(S::NS - 1) * LOADS>();
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int i = 0; i < TM; ++i) read_x(i, 0, smem);
+
+    int stage = 0;                                // of the current 64 k, in bytes
+    for (int kb = 0; kb < nk; ++kb) {
+        load_codes(next, words_next, kb0 + kb + 1);
+        auto step = [&](auto j_c) {
+            constexpr int j = decltype(j_c)::value, half = j & 1;
+            unsigned char* s = smem + stage;
+            const int after = stage == (S::NS - 1) * S::STAGE ? 0 : stage + S::STAGE;
+            unsigned char* sn = smem + after;
+            constexpr int BAR = 2;                // second half: reads start behind the barrier, which is in front of this fragment
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                if (half && i == BAR) {
+                    __builtin_amdgcn_s_waitcnt(0xC07F);                // lgkmcnt(0): this wave has read what it reads of the stage
+                    // The next stage has landed: behind it only the one after it was requested for certain (the compiler is free to
+                    // move the loads of codes, which can only make this wait longer).
+                    wait_vmcnt<LOADS>();
+                    __builtin_amdgcn_s_barrier();
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    acc[i][f] = mfma16(operand(fw[half][f]), fx[i], acc[i][f]);
+                    const int slot = i * 4 + f;
+                    constexpr int EVERY = TM / 4;
+                    if (slot % EVERY == EVERY - 1) {
+                        if (j == 3) make(fw[0], next, words_next, 0, slot / EVERY);
+                        else make(fw[1 - half], now, words_now, j + 1, slot / EVERY);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (!half) {
+                    read_x(i, 1, s);
+                } else if (i >= BAR) {
+                    if (i == BAR) {
+#pragma unroll
+                        for (int q = 0; q < BAR; ++q) read_x(q, 0, sn);
+                    }
+                    read_x(i, 0, sn);
+                    // the stage's loads, dealt over the rest of the step
+#pragma unroll
+                    for (int n = 0; n < LOADS; ++n)
+                        if (BAR + n * (TM - BAR) / LOADS == i) load_x(n, (kb0 + kb) * 2 + (j >> 1) + S::NS, s);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (TRANSPOSED) load_words(kb0 + kb + (j >= 2 ? 1 : 0), (j + 2) & 3);
+            if (half) stage = after;
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+        step(std::integral_constant<int, 2>());
+        step(std::integral_constant<int, 3>());
+#pragma unroll
+        for (int f = 0; f < 4; ++f) now[f] = next[f];
+        words_now = words_next;
+    }
+    wait_vmcnt<0>();                              // no load into LDS outlives the workgroup
+    if (!there) return;
+
+    // lane: token l % 16 of fragment i, features 4 * (l / 16) .. + 3 of fragment f
+    const int64_t row0 = int64_t(row_tile) * S::BM;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int64_t token = row0 + i * 16 + r;
+        if (token >= a.tokens) continue;
+        if constexpr (FORM == INT4_PARTIAL) {
+            float* p = a.partial + (int64_t(split) * a.tokens + token) * a.ld + first * kPiece + kq * 4;
+#pragma unroll
+            for (int f = 0; f < 4; ++f) *reinterpret_cast<floatx4*>(p + f * kPiece) = acc[i][f];
+        } else {
+            const int tensor = FORM == INT4_GATED ? 0 : first / a.f_pieces, f0 = (first - tensor * a.f_pieces) * kPiece + kq * 4;
+            bf16_t* y = a.y + token * a.y_stride + int64_t(tensor) * a.features + f0;
+#pragma unroll
+            for (int f = 0; f < (FORM == INT4_GATED ? 2 : 4); ++f) {
+                floatx4 v = acc[i][f];
+                if constexpr (FORM == INT4_GATED) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[q] = gated_value(v[q], acc[i][f + 2][q]);
+                }
+                const int n = a.features - f0 - f * kPiece;
+                if (n > 0) store4(y + f * kPiece, n, v);
+            }
+        }
+    }
+}
+#endif
+
+template <int TM, int FORM, bool TRANSPOSED, int SUB>
+__global__ void __launch_bounds__(256, Int4Shape<TM>::PER_CU) int4_gemm_kernel(Int4GemmArgs g) {
+#ifdef __HIP_DEVICE_COMPILE__
+    int4_tile<TM, FORM, TRANSPOSED, SUB>(g);
+#endif
+}
+
+// The ranges of K added up in order: a thread takes 4 neighbouring features of a token. Gated: of gate and of up, then silu(gate) * up.
+template <bool GATED>
+__global__ void __launch_bounds__(256) int4_reduce_kernel(Int4Args a) {
+    const int64_t per_token = (GATED ? a.ld / 2 : a.ld) / 4, all = a.tokens * per_token, step = a.tokens * a.ld;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+        const int64_t token = i / per_token;
+        const int f4 = int(i - token * per_token) * 4, tensor = f4 / (a.f_pieces * kPiece), f = f4 - tensor * a.f_pieces * kPiece;
+        if (f >= a.features) continue;
+        auto sum = [&](int at) {
+            const float* p = a.partial + token * a.ld + at;
+            floatx4 v = *reinterpret_cast<const floatx4*>(p);
+            for (int s = 1; s < a.n_split; ++s) v += *reinterpret_cast<const floatx4*>(p + s * step);
+            return v;
+        };
+        floatx4 v = sum(f4);
+        if constexpr (GATED) {
+            const floatx4 up = sum(f4 + int(a.ld / 2));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = gated_value(v[q], up[q]);
+        }
+        store4(a.y + token * a.y_stride + int64_t(tensor) * a.features + f, a.features - f, v);
+    }
+}

@@ -1,0 +1,405 @@
+// Projections with frozen 4-bit weights (include/tn_int4.h): host side and C ABI. Kernels: kernels/int4_*.hpp.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <new>
+#include <utility>
+
+#include "../../include/tn_fp8.h"
+#include "../../include/tn_int4.h"
+
+namespace {
+
+#include "kernels/fp8_format.hpp"
+#include "kernels/int4_weight.hpp"
+#include "kernels/int4_stream.hpp"
+#include "kernels/int4_gemm.hpp"
+
+constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxStride = int64_t(1) << 22;
+constexpr int kCUs = 256, kBand = 5;
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+int launched() { return hipGetLastError() == hipSuccess ? TN_OK : TN_ERR_HIP; }
+int64_t whole(int64_t bytes) { return div_up(bytes, 256) * 256; }
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p < q + uintptr_t(b_bytes) && q < p + uintptr_t(a_bytes);
+}
+
+}  // namespace
+
+struct tn_int4_linear_s {
+    int32_t tensors = 1, transpose = 0, group = 128;
+    int64_t m = 0, n = 0, groups = 0;     // of each tensor
+    int32_t features = 0;                 // outputs of one of `out_segments` runs of features
+    int32_t out_segments = 1, k_segments = 1;
+    int64_t k_cols = 0;                   // inputs: segments of k_cols
+    int64_t f_pieces = 0, own_k_blocks = 0, k_blocks = 0;
+    unsigned *packed = nullptr, *words = nullptr;
+    int64_t packed_bytes = 0, word_bytes = 0, word_stride = 0;
+    ~tn_int4_linear_s() {
+        if (packed) (void)hipFree(packed);
+        if (words) (void)hipFree(words);
+    }
+};
+
+namespace {
+
+int check_desc(const tn_int4_linear_desc& d) {
+    if (d.out_features < 1 || d.in_features < 1 || d.n_tensors < 1 || d.n_tensors > 2 || (d.flags & ~TN_FLAG_TRANSPOSE)) return TN_ERR_INVALID_ARG;
+    if (d.group != 32 && d.group != 64 && d.group != 128) return TN_ERR_INVALID_ARG;
+    if (d.dtype != TN_DTYPE_INT4 && d.dtype != TN_DTYPE_F32 && d.dtype != TN_DTYPE_BF16) return TN_ERR_INVALID_ARG;
+    if (d.dtype == TN_DTYPE_INT4 && d.scale_dtype != TN_DTYPE_BF16 && d.scale_dtype != TN_DTYPE_F16) return TN_ERR_INVALID_ARG;
+    return d.out_features > TN_INT4_MAX_FEATURES || d.in_features > TN_INT4_MAX_FEATURES ? TN_ERR_UNSUPPORTED : TN_OK;
+}
+
+void lay_out(const tn_int4_linear_desc& d, tn_int4_linear_s& h) {
+    h.tensors = d.n_tensors;
+    h.transpose = (d.flags & TN_FLAG_TRANSPOSE) ? 1 : 0;
+    h.group = d.group;
+    h.m = d.out_features;
+    h.n = d.in_features;
+    h.groups = div_up(h.n, h.group);
+    h.features = int32_t(h.transpose ? h.n : h.m);
+    h.f_pieces = div_up(h.features, kFeaturePad) * (kFeaturePad / kPiece);
+    h.out_segments = h.transpose ? 1 : h.tensors;
+    h.k_cols = h.transpose ? h.m : h.n;
+    h.k_segments = h.transpose ? h.tensors : 1;
+    h.own_k_blocks = div_up(h.k_cols, kBlock);
+    h.k_blocks = h.k_segments * h.own_k_blocks;
+    h.packed_bytes = h.out_segments * h.f_pieces * h.k_blocks * kPieceWords * 4;
+    h.word_stride = h.k_blocks * kBlock;
+    h.word_bytes = 4 * (h.transpose ? div_up(h.f_pieces * kPiece, h.group) * h.word_stride
+                                    : h.out_segments * h.f_pieces * h.k_blocks * (kBlock / h.group) * kPiece);
+}
+
+OperandArgs operand_args(const tn_int4_linear_s& h, int slot) {
+    OperandArgs a{};
+    a.packed = h.packed;
+    a.words = h.words;
+    a.m = h.m;
+    a.n = h.n;
+    a.groups = h.groups;
+    a.group = h.group;
+    a.transpose = h.transpose;
+    a.k_blocks = int32_t(h.k_blocks);
+    a.sub = kBlock / h.group;
+    a.piece0 = h.transpose ? 0 : slot * h.f_pieces;
+    a.k_block0 = h.transpose ? slot * h.own_k_blocks : 0;
+    a.f_pieces = h.f_pieces;
+    a.own_k_blocks = h.own_k_blocks;
+    a.word_stride = h.word_stride;
+    return a;
+}
+
+Int4Args product_args(const tn_int4_linear_s& h, const void* x, int64_t x_stride, int64_t tokens) {
+    Int4Args a{};
+    a.x = static_cast<const bf16_t*>(x);
+    a.x_stride = x_stride;
+    a.packed = h.packed;
+    a.words = h.words;
+    a.tokens = tokens;
+    a.word_stride = h.word_stride;
+    a.k_blocks = int32_t(h.k_blocks);
+    a.sub = kBlock / h.group;
+    a.features = h.features;
+    a.f_pieces = int32_t(h.f_pieces);
+    a.tensors = h.out_segments;
+    a.group_pieces = h.group / kPiece;
+    a.transpose = h.transpose;
+    a.n_split = 1;
+    a.ld = h.out_segments * h.f_pieces * kPiece;
+    return a;
+}
+
+// ---------------------------------------------------------------------------------------------
+// which kernel a product runs on
+// ---------------------------------------------------------------------------------------------
+constexpr int64_t kStreamTokens = 64;           // streamed up to here
+constexpr int kTileTokens[] = {4, 8, 16};       // TM
+
+struct Choice {
+    int tm = 0;                // tile of 16 * tm tokens; 0: streamed
+    int split = 1;
+    int groups = 2, tg = 1;    // streamed: pieces and 16s of tokens to a workgroup
+};
+
+Choice choose(const Int4Args& a, bool gated) {
+    Choice c;
+    const int64_t pieces = int64_t(a.f_pieces) * a.tensors;
+    if (a.tokens <= kStreamTokens) {
+        c.tg = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+        return c;
+    }
+    const int64_t n_col = div_up(gated ? pieces / 2 : pieces, gated ? 8 : 16);
+    double best = 1e30;
+    for (const int tm : kTileTokens) {
+        const int64_t n_row = div_up(a.tokens, 16 * tm);
+        for (const int split : {1, 2, 3, 4, 6, 8}) {
+            if (split > 1 && split * 4 > a.k_blocks) break;
+            const int64_t blocks = div_up(a.k_blocks, split), items = n_row * n_col * div_up(a.k_blocks, blocks);
+            const int per_cu = tm <= 8 ? 2 : 1;
+            const double k_block = tm == 4 ? 0.62 : tm == 8 ? 1.15 : 2.0;          // us of a workgroup, with per_cu on a CU
+            double us = div_up(items, kCUs * per_cu) * (blocks * k_block + 3.0);
+            if (split > 1) us += 4.0 + double(a.tokens) * a.ld * 4 * 2 * split / 5e6;
+            if (us < best) {
+                best = us;
+                c.tm = tm;
+                c.split = split;
+            }
+        }
+    }
+    return c;
+}
+
+// Waves of a workgroup of the stream kernel: the number up to 8 that leaves the fewest of them idle in the last round
+int stream_waves(int k_blocks, int blocks) {
+    const int rounds = int(div_up(k_blocks, blocks));
+    int best = rounds < 8 ? rounds : 8;
+    for (int w = best - 1; w >= 4; --w)
+        if (div_up(rounds, w) * w < div_up(rounds, best) * best) best = w;
+    return best;
+}
+
+template <int GROUPS, int TG, int SUB, bool TRANSPOSED, bool GATED>
+int run_stream(const Int4Args& a, hipStream_t stream) {
+    constexpr int OWN = GATED ? GROUPS / 2 : GROUPS, BLOCKS = TG == 1 ? 4 : TG == 2 ? 2 : 1;
+    const dim3 grid(unsigned((GATED ? a.f_pieces : int64_t(a.f_pieces) * a.tensors) / OWN), unsigned(div_up(a.tokens, 16 * TG)));
+    int4_stream_kernel<GROUPS, TG, SUB, TRANSPOSED, GATED><<<grid, dim3(64 * stream_waves(a.k_blocks, BLOCKS)), 0, stream>>>(a);
+    return launched();
+}
+template <int GROUPS, int TG>
+int stream_form(const Int4Args& a, bool gated, hipStream_t stream) {
+    if (a.transpose) return run_stream<GROUPS, TG, 1, true, false>(a, stream);
+    switch (a.sub) {
+        case 1: return gated ? run_stream<GROUPS, TG, 1, false, true>(a, stream) : run_stream<GROUPS, TG, 1, false, false>(a, stream);
+        case 2: return gated ? run_stream<GROUPS, TG, 2, false, true>(a, stream) : run_stream<GROUPS, TG, 2, false, false>(a, stream);
+        default: return gated ? run_stream<GROUPS, TG, 4, false, true>(a, stream) : run_stream<GROUPS, TG, 4, false, false>(a, stream);
+    }
+}
+
+template <int TM, int FORM, bool TRANSPOSED, int SUB>
+int run_gemm(const Int4GemmArgs& g, hipStream_t stream) {
+    const int64_t items = int64_t(g.n_row) * g.n_col * g.l.n_split;
+    int4_gemm_kernel<TM, FORM, TRANSPOSED, SUB><<<dim3(unsigned(div_up(items, 8) * 8)), dim3(256), Int4Shape<TM>::SMEM, stream>>>(g);
+    return launched();
+}
+template <int TM, int FORM>
+int gemm_form(const Int4GemmArgs& g, hipStream_t stream) {
+    if constexpr (FORM != INT4_GATED) {
+        if (g.l.transpose) return g.l.group_pieces >= 4 ? run_gemm<TM, FORM, true, 1>(g, stream) : run_gemm<TM, FORM, true, 2>(g, stream);
+    }
+    return g.l.sub == 1 ? run_gemm<TM, FORM, false, 1>(g, stream) : g.l.sub == 2 ? run_gemm<TM, FORM, false, 2>(g, stream) : run_gemm<TM, FORM, false, 4>(g, stream);
+}
+template <int TM>
+int run_tiles(const Int4Args& a, bool gated, hipStream_t stream) {
+    Int4GemmArgs g{};
+    g.l = a;
+    g.blocks_per_split = int(div_up(a.k_blocks, a.n_split));
+    g.l.n_split = int(div_up(a.k_blocks, g.blocks_per_split));         // no range without a block
+    const bool fused = gated && !a.partial;
+    const int64_t pieces = int64_t(a.f_pieces) * a.tensors;
+    const int64_t n_row = div_up(a.tokens, 16 * TM), n_col = fused ? div_up(a.f_pieces, 8) : div_up(pieces, 16);
+    if (n_row * n_col * g.l.n_split > INT32_MAX / 8) return TN_ERR_UNSUPPORTED;
+    g.n_row = int(n_row);
+    g.n_col = int(n_col);
+    g.band = int(div_up(n_row, div_up(n_row, kBand)));
+    int rc = fused ? gemm_form<TM, INT4_GATED>(g, stream) : a.partial ? gemm_form<TM, INT4_PARTIAL>(g, stream) : gemm_form<TM, INT4_PLAIN>(g, stream);
+    if (rc != TN_OK || !a.partial) return rc;
+    const int64_t blocks = div_up(a.tokens * (gated ? a.ld / 2 : a.ld) / 4, 256);
+    const dim3 grid(unsigned(blocks < 8 * kCUs ? blocks : 8 * kCUs));
+    if (gated) int4_reduce_kernel<true><<<grid, dim3(256), 0, stream>>>(g.l);
+    else int4_reduce_kernel<false><<<grid, dim3(256), 0, stream>>>(g.l);
+    return launched();
+}
+
+template <int TM, int FORM, bool TRANSPOSED, int SUB>
+bool allow() {          // more LDS than a launch gets by default
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(int4_gemm_kernel<TM, FORM, TRANSPOSED, SUB>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               Int4Shape<TM>::SMEM) == hipSuccess;
+}
+template <int TM>
+bool allow_tiles() {
+    return allow<TM, INT4_PLAIN, false, 1>() && allow<TM, INT4_PLAIN, false, 2>() && allow<TM, INT4_PLAIN, false, 4>() && allow<TM, INT4_PLAIN, true, 1>() &&
+           allow<TM, INT4_PLAIN, true, 2>() && allow<TM, INT4_PARTIAL, false, 1>() && allow<TM, INT4_PARTIAL, false, 2>() &&
+           allow<TM, INT4_PARTIAL, false, 4>() && allow<TM, INT4_PARTIAL, true, 1>() && allow<TM, INT4_PARTIAL, true, 2>() &&
+           allow<TM, INT4_GATED, false, 1>() && allow<TM, INT4_GATED, false, 2>() && allow<TM, INT4_GATED, false, 4>();
+}
+
+// Rows that the products cannot read where they are
+bool laid_out_anew(const tn_int4_linear_s& h, const void* x, int64_t x_stride) {
+    return h.k_cols % kBlock != 0 || !aligned(x, 16) || x_stride % kChunk != 0 || x_stride >= kMaxStride;
+}
+struct Workspace {
+    int64_t rows = 0, sums = 0;
+};
+Workspace workspace_of(const tn_int4_linear_s& h, const void* x, int64_t x_stride, int64_t tokens, bool gated) {
+    Workspace w;
+    if (laid_out_anew(h, x, x_stride)) w.rows = whole(tokens * h.k_blocks * kBlock * 2);
+    const Int4Args a = product_args(h, x, x_stride, tokens);
+    const Choice c = choose(a, gated);
+    if (c.tm && c.split > 1) w.sums = whole(c.split * tokens * a.ld * 4);
+    return w;
+}
+
+int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t tokens, bool gated, void* workspace,
+                int64_t workspace_bytes, hipStream_t stream) {
+    if (tokens < 0) return TN_ERR_INVALID_ARG;
+    if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    if (tokens == 0) return TN_OK;
+    const int64_t x_cols = h.k_segments * h.k_cols, y_cols = gated ? h.features : int64_t(h.out_segments) * h.features;
+    if (!x || !y || x_stride < x_cols || y_stride < y_cols || !aligned(x, 2) || !aligned(y, 2)) return TN_ERR_INVALID_ARG;
+    // workgroups read rows of x while others write theirs of y
+    if (overlap(x, ((tokens - 1) * x_stride + x_cols) * 2, y, ((tokens - 1) * y_stride + y_cols) * 2)) return TN_ERR_INVALID_ARG;
+    const Workspace w = workspace_of(h, x, x_stride, tokens, gated);
+    if (w.rows + w.sums > 0 && (!workspace || workspace_bytes < w.rows + w.sums || !aligned(workspace, 256))) return TN_ERR_INVALID_ARG;
+    if (w.rows) {
+        bf16_t* rows = static_cast<bf16_t*>(workspace);
+        const int64_t blocks = div_up(tokens * h.k_blocks * (kBlock / kChunk), 256);
+        int4_rows_kernel<<<dim3(unsigned(blocks < 32 * kCUs ? blocks : 32 * kCUs)), dim3(256), 0, stream>>>(
+            static_cast<const bf16_t*>(x), x_stride, tokens, h.k_segments, h.k_cols, h.own_k_blocks * kBlock, rows);
+        const int rc = launched();
+        if (rc != TN_OK) return rc;
+        x = rows;
+        x_stride = h.k_blocks * kBlock;
+    }
+    Int4Args a = product_args(h, x, x_stride, tokens);
+    a.y = static_cast<bf16_t*>(y);
+    a.y_stride = y_stride;
+    const Choice c = choose(a, gated);
+    if (c.tm == 0) return c.tg == 1 ? stream_form<2, 1>(a, gated, stream) : c.tg == 2 ? stream_form<2, 2>(a, gated, stream) : stream_form<2, 4>(a, gated, stream);
+    a.n_split = c.split;
+    if (c.split > 1) a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.rows);
+    return c.tm == 4 ? run_tiles<4>(a, gated, stream) : c.tm == 8 ? run_tiles<8>(a, gated, stream) : run_tiles<16>(a, gated, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tn_int4_linear_create(tn_int4_linear_t* out, const tn_int4_linear_desc* d) {
+    if (!out || !d || !d->tensors) return TN_ERR_INVALID_ARG;
+    const int bad = check_desc(*d);
+    if (bad != TN_OK) return bad;
+    const bool given = d->dtype == TN_DTYPE_INT4;
+    if (given && !d->scales) return TN_ERR_INVALID_ARG;
+    for (int i = 0; i < d->n_tensors; ++i)
+        if (!d->tensors[i] || (given && (!d->scales[i] || !aligned(d->scales[i], 2) || (d->zeros && !d->zeros[i]))) ||
+            (!given && !aligned(d->tensors[i], d->dtype == TN_DTYPE_F32 ? 4 : 2)))
+            return TN_ERR_INVALID_ARG;
+    tn_int4_linear_s* h = new (std::nothrow) tn_int4_linear_s;
+    if (!h) return TN_ERR_ALLOC;
+    lay_out(*d, *h);
+    const hipStream_t st = static_cast<hipStream_t>(d->stream);
+    const int64_t row_bytes = div_up(h->n, 2);
+    int rc = allow_tiles<4>() && allow_tiles<8>() && allow_tiles<16>() ? TN_OK : TN_ERR_HIP;
+    // (what is quantised here passes through the form that a caller gives)
+    unsigned char* made = nullptr;
+    const int64_t scales_at = whole(h->m * row_bytes), zeros_at = scales_at + whole(h->m * h->groups * 2);
+    if (rc == TN_OK && (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
+                        hipMalloc(reinterpret_cast<void**>(&h->words), size_t(h->word_bytes)) != hipSuccess ||
+                        (!given && hipMalloc(reinterpret_cast<void**>(&made), size_t(zeros_at + h->m * h->groups)) != hipSuccess))) {
+        (void)hipGetLastError();
+        rc = TN_ERR_ALLOC;
+    }
+    for (int i = 0; rc == TN_OK && i < h->tensors; ++i) {
+        OperandArgs a = operand_args(*h, i);
+        if (given) {
+            a.codes = static_cast<const unsigned char*>(d->tensors[i]);
+            a.scales = d->scales[i];
+            a.zeros = d->zeros ? static_cast<const unsigned char*>(d->zeros[i]) : nullptr;
+            a.scale_f16 = d->scale_dtype == TN_DTYPE_F16;
+        } else {
+            const dim3 grid(unsigned(div_up(h->m * h->groups, 256)));
+            bf16_t* scales = reinterpret_cast<bf16_t*>(made + scales_at);
+            if (d->dtype == TN_DTYPE_F32)
+                int4_quantise_kernel<float><<<grid, dim3(256), 0, st>>>(static_cast<const float*>(d->tensors[i]), h->m, h->n, h->groups, h->group, made, scales, made + zeros_at);
+            else
+                int4_quantise_kernel<bf16_t><<<grid, dim3(256), 0, st>>>(static_cast<const bf16_t*>(d->tensors[i]), h->m, h->n, h->groups, h->group, made, scales, made + zeros_at);
+            a.codes = made;
+            a.scales = scales;
+            a.zeros = made + zeros_at;
+        }
+        int4_pack_kernel<<<dim3(unsigned(h->f_pieces), unsigned(h->own_k_blocks)), dim3(256), 0, st>>>(a);
+        const int64_t words = h->transpose ? div_up(h->f_pieces * kPiece, h->group) * h->own_k_blocks * kBlock
+                                           : h->f_pieces * h->own_k_blocks * a.sub * kPiece;
+        int4_words_kernel<<<dim3(unsigned(div_up(words, 256))), dim3(256), 0, st>>>(a);
+        rc = launched();
+    }
+    if (rc == TN_OK && hipStreamSynchronize(st) != hipSuccess) rc = TN_ERR_HIP;
+    if (made) {
+        if (rc != TN_OK) (void)hipStreamSynchronize(st);
+        (void)hipFree(made);
+    }
+    if (rc != TN_OK) {
+        delete h;
+        return rc;
+    }
+    *out = h;
+    return TN_OK;
+}
+
+int64_t tn_int4_linear_workspace(tn_int4_linear_t h, const void* x, int64_t x_stride, int64_t tokens, int32_t gated) {
+    if (!h || tokens < 0 || (gated && h->out_segments != 2)) return TN_ERR_INVALID_ARG;
+    if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    if (tokens == 0) return 0;
+    const Workspace w = workspace_of(*h, x, x_stride, tokens, gated != 0);
+    return w.rows + w.sums;
+}
+
+int tn_int4_linear_forward(tn_int4_linear_t h, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t tokens, void* workspace,
+                           int64_t workspace_bytes, void* stream) {
+    if (!h) return TN_ERR_INVALID_ARG;
+    return run_product(*h, x, x_stride, y, y_stride, tokens, false, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int tn_int4_linear_gated(tn_int4_linear_t h, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t tokens, void* workspace,
+                         int64_t workspace_bytes, void* stream) {
+    if (!h || h->out_segments != 2) return TN_ERR_INVALID_ARG;
+    return run_product(*h, x, x_stride, y, y_stride, tokens, true, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+int tn_int4_linear_plan_query(const tn_int4_linear_desc* d, int64_t tokens, int32_t gated, int32_t what, int64_t* value) {
+    if (!d || !value || tokens < 1 || (gated && (d->n_tensors != 2 || (d->flags & TN_FLAG_TRANSPOSE)))) return TN_ERR_INVALID_ARG;
+    const int bad = check_desc(*d);
+    if (bad != TN_OK) return bad;
+    if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
+    tn_int4_linear_s h;
+    lay_out(*d, h);
+    const Choice c = choose(product_args(h, nullptr, 0, tokens), gated != 0);
+    switch (what) {
+        case TN_INT4_PLAN_TILE_TOKENS: *value = 16 * c.tm; return TN_OK;
+        case TN_INT4_PLAN_RANGES: *value = c.split; return TN_OK;
+        case TN_INT4_PLAN_STREAM_TOKENS: *value = c.tm ? 0 : 16 * c.tg; return TN_OK;
+        case TN_INT4_PLAN_STREAM_PIECES: *value = c.tm ? 0 : c.groups; return TN_OK;
+        default: return TN_ERR_INVALID_ARG;
+    }
+}
+
+int tn_int4_linear_tensor(tn_int4_linear_t h, int32_t slot, void* codes, void* scales, void* zeros, void* stream) {
+    if (!h || slot < 0 || slot >= h->tensors || !aligned(scales, 4)) return TN_ERR_INVALID_ARG;
+    if (!codes && !scales && !zeros) return TN_OK;
+    const dim3 grid(unsigned(div_up(div_up(h->n, 2), 256)), unsigned(h->m < 65535 ? h->m : 65535), unsigned(div_up(h->m, 65535)));
+    int4_unpack_kernel<<<grid, dim3(256), 0, static_cast<hipStream_t>(stream)>>>(operand_args(*h, slot), static_cast<unsigned char*>(codes),
+                                                                                 static_cast<float*>(scales), static_cast<unsigned char*>(zeros));
+    return launched();
+}
+
+int tn_int4_linear_query(tn_int4_linear_t h, int32_t what, int64_t* value) {
+    if (!h || !value) return TN_ERR_INVALID_ARG;
+    switch (what) {
+        case TN_QUERY_OUT_FEATURES: *value = int64_t(h->out_segments) * h->features; return TN_OK;
+        case TN_QUERY_IN_FEATURES: *value = h->k_segments * h->k_cols; return TN_OK;
+        case TN_QUERY_PARAM_COUNT: *value = h->tensors * h->m * h->n; return TN_OK;
+        case TN_QUERY_PACKED_BYTES: *value = h->packed_bytes + h->word_bytes; return TN_OK;
+        default: return TN_ERR_INVALID_ARG;
+    }
+}
+
+int tn_int4_linear_destroy(tn_int4_linear_t h) {
+    delete h;
+    return TN_OK;
+}
+
+}  // extern "C"

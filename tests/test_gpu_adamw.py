@@ -1,0 +1,296 @@
+"""The AdamW step over many tensors and the norm of their gradients against 64 bits. The oracle is oracle/adamw_oracle.py."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.adamw_oracle as O
+import paper_2602_01613_amd as tn
+from fp8_util import exponents, half_unit, host
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [1, 7, 128, 129, 0, 5000, 127, 4096, 4097, 2, 20001, 256]
+MANY = [1 + (i * 37) % 300 for i in range(600)]
+BETAS, EPS, LR, DECAY = (0.9, 0.999), 1e-8, 1e-3, 0.02
+
+
+def places(sizes):
+    at, result = 0, []
+    for n in sizes:
+        result.append(at)
+        at += -(-n // 128) * 128
+    return result, at
+
+
+class Setup:
+    """Parameters that lie anywhere in a buffer (odd offsets), gradients likewise, and the same in 64 bits, laid out like the state."""
+
+    def __init__(self, sizes, params, grads, bits, seed=0, **more):
+        rng = np.random.default_rng(seed)
+        self.rng, self.sizes, self.bits = rng, sizes, bits
+        self.places, self.length = places(sizes)
+        kinds = lambda which: [torch.bfloat16 if which == "bf16" or (which == "mixed" and i % 3 == 1) else torch.float32 for i in range(len(sizes))]      # noqa: E731
+        self.params = [self.tensor(n, k, 0.05) for n, k in zip(sizes, kinds(params))]
+        self.grad_kinds = kinds(grads)
+        self.around = [b.clone() for _, b in self.params]
+        self.opt = tn.AdamW([p for p, _ in self.params], lr=LR, betas=BETAS, eps=EPS, weight_decay=more.pop("weight_decay", DECAY), state_bits=bits, seed=77, **more)
+        self.new_gradients()
+
+    def tensor(self, n, dtype, size):
+        lead = int(self.rng.integers(1, 5))
+        buffer = torch.from_numpy(self.rng.standard_normal(n + lead + 3) * size).to(dtype).cuda()
+        return buffer[lead:lead + n], buffer
+
+    def new_gradients(self, size=1e-2):
+        self.grads = [self.tensor(n, k, size)[0] for n, k in zip(self.sizes, self.grad_kinds)]
+
+    def flat(self, tensors):
+        out = np.zeros(self.length)
+        for t, p, n in zip(tensors, self.places, self.sizes):
+            out[p:p + n] = host(t)
+        return out
+
+    def values(self):
+        """Parameters as the step reads them: the masters where there are any."""
+        out = self.flat([p for p, _ in self.params])
+        if "master" in self.opt.state_dict():
+            master = host(self.opt.state_dict()["master"])
+            for (t, _), p, n in zip(self.params, self.places, self.sizes):
+                if t.dtype == torch.bfloat16:
+                    out[p:p + n] = master[p:p + n]
+        return out
+
+    def states(self):
+        s = self.opt.state_dict()
+        if self.bits == 32:
+            return host(s["first"]), host(s["second"])
+        value = lambda k: host(s[k]) * np.repeat(np.exp2(exponents(s[k + "_scales"]).astype(np.float64)), 128)      # noqa: E731
+        return value("first"), value("second") ** 2
+
+    def check_around(self):
+        """Nothing beside a parameter was written, and a bf16 parameter is its master rounded."""
+        master = self.opt.state_dict().get("master")
+        for (t, b), before, p, n in zip(self.params, self.around, self.places, self.sizes):
+            lead = t.storage_offset()
+            assert torch.equal(b[:lead], before[:lead]) and torch.equal(b[lead + n:], before[lead + n:])
+            if t.dtype == torch.bfloat16:
+                assert torch.equal(master[p:p + n].bfloat16(), t)
+
+
+def check_step(s, before, states, t, got_states, clip=1.0, decay=DECAY, lr=LR):
+    """fp32: a handful of roundings of 2^-24 for each of m, v and the parameter, the last one also with those of its move (hardware division and
+    root: 2^-22), of which there are fewer than 16."""
+    p, m, v = O.step(before, s.flat(s.grads), *states, t, lr, *BETAS, EPS, decay, clip)
+    g = np.abs(s.flat(s.grads)) * clip
+    off_m = 2.0 ** -22 * (np.abs(states[0]) + g)
+    off_v = 2.0 ** -21 * v
+    now = s.values()
+    assert (np.abs(now - p) <= 2.0 ** -22 * np.abs(before) + 2.0 ** -18 * np.abs(p - before * (1 - lr * np.asarray(decay))) + lr * off_m / (1 - BETAS[0] ** t) / (np.sqrt(v) + EPS) + 1e-30).all()
+    if s.bits == 32:
+        assert (np.abs(got_states[0] - m) <= off_m).all() and (np.abs(got_states[1] - v) <= off_v).all()
+        return
+    h = O.hash_of(77, t, np.arange(s.length))
+    for got, exact, off, bits, key in ((got_states[0], m, off_m, h & np.uint64(0xFFFF), "first"), (np.sqrt(got_states[1]), np.sqrt(v), 2.0 ** -21 * np.sqrt(v), h >> np.uint64(16), "second")):
+        codes, e = O.quantize(exact, bits)
+        got_e = exponents(s.opt.state_dict()[key + "_scales"])
+        ref = (codes.reshape(-1, 128) * np.exp2(e.astype(np.float64))[:, None]).reshape(-1)
+        _, _, _, _, step = O.neighbours(exact)
+        step = (step * np.exp2(e.astype(np.float64))[:, None]).reshape(-1)
+        # the same codes, but where fp32's error moves the value past the point at which the random number decides, and then the neighbouring one
+        same = np.repeat(e == got_e, 128)
+        assert (np.abs(got - ref)[same] <= 1.001 * step[same]).all()
+        differ = (got != ref)
+        # off / step of the values cross the threshold; below the least normal code 2^-20 of a step are rounded before it
+        assert differ[same].mean() <= 4 * (off / step + 2.0 ** -20).mean() + 20 / s.length
+        assert (e != got_e).sum() <= 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("params,grads", [("f32", "f32"), ("bf16", "f32"), ("mixed", "mixed"), ("bf16", "bf16")])
+@pytest.mark.parametrize("sizes", [SIZES, MANY, [1], [300000]], ids=["odd", "many", "one", "long"])
+def test_steps(sizes, params, grads, bits):
+    s = Setup(sizes, params, grads, bits)
+    for t in range(1, 5):
+        before, states = s.values(), s.states()
+        assert s.opt.step(s.grads) is None
+        check_step(s, before, states, t, s.states())
+        s.check_around()
+        assert int(s.opt.state_dict()["count"]) == t
+        s.new_gradients(10.0 ** -t)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_clipping(bits):
+    s = Setup(SIZES, "mixed", "mixed", bits)
+    for t, (max_norm, given) in enumerate([(0.1, False), (1e3, False), (0.1, True)], 1):
+        before, states = s.values(), s.states()
+        n = np.sqrt((s.flat(s.grads) ** 2).sum())
+        known = torch.tensor(2 * n, dtype=torch.float32, device="cuda") if given else None
+        got = s.opt.step(s.grads, max_norm=max_norm, norm=known)
+        if given:
+            assert got is known
+            n = float(known)
+        assert abs(float(got) - n) <= 2.0 ** -23 * n
+        check_step(s, before, states, t, s.states(), clip=min(1.0, max_norm / float(got)))
+
+
+@pytest.mark.parametrize("grads", ["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("sizes", [SIZES, MANY, [1], [0], [3000000]], ids=["odd", "many", "one", "none", "long"])
+def test_norm(sizes, grads):
+    """Summed in 64 bits and rounded once: half a unit of fp32."""
+    s = Setup(sizes, "f32", grads, 32)
+    for size in (1e-2, 1e25, 1e-30):
+        s.new_gradients(size)
+        n = np.sqrt((s.flat(s.grads) ** 2).sum())
+        got = s.opt.gradient_norm(s.grads)
+        assert got.dtype == torch.float32 and got.dim() == 0
+        assert abs(float(got) - n) <= half_unit(n, "f32") * (1 + 1e-6) + 1e-45
+        assert torch.equal(s.opt.gradient_norm(s.grads), got)
+    out = torch.zeros((), device="cuda")
+    assert s.opt.gradient_norm(s.grads, out=out) is out and torch.equal(out, got)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_a_norm_that_is_not_finite_changes_nothing(bits, bad):
+    s = Setup(SIZES, "mixed", "f32", bits)
+    s.opt.step(s.grads)
+    before = {k: v.clone() for k, v in s.opt.state_dict().items()}
+    params = [p.clone() for p, _ in s.params]
+    s.grads[5][4999] = bad
+    assert not np.isfinite(float(s.opt.step(s.grads, max_norm=1.0)))
+    for k, v in s.opt.state_dict().items():
+        assert torch.equal(v.view(torch.uint8) if v.dim() else v, before[k].view(torch.uint8) if v.dim() else before[k]), k
+    assert all(torch.equal(p, q) for (p, _), q in zip(s.params, params))
+
+
+def test_what_is_not_finite_stays_where_it_is():
+    """Without clipping a NaN or an infinity reaches its own value of the parameter and the state, and no other: in 8 bits it is a NaN code, out of
+    the scale of its block."""
+    for bits in (32, 8):
+        s, clean = (Setup([300], "f32", "f32", bits, seed=3) for _ in range(2))
+        s.grads[0][5], s.grads[0][200] = float("nan"), float("inf")
+        s.opt.step(s.grads)
+        clean.opt.step(clean.grads)
+        got, ref = s.values(), clean.values()
+        bad = np.zeros(s.length, dtype=bool)
+        bad[[5, 200]] = True
+        assert np.isnan(got[bad]).all() and np.array_equal(got[~bad], ref[~bad])
+        for a, b in zip(s.states(), clean.states()):
+            assert not np.isfinite(a[bad]).any() and np.isfinite(a[~bad]).all()
+            if bits == 32:
+                assert np.array_equal(a[~bad], b[~bad])
+
+
+def test_each_tensor_has_its_decay():
+    s = Setup([100, 200, 300], "f32", "f32", 32, weight_decay=[0.0, 0.5, 0.1])
+    before, states = s.values(), s.states()
+    s.opt.step(s.grads, lr=0.01)
+    decay = np.zeros(s.length)
+    for p, n, d in zip(s.places, s.sizes, (0.0, 0.5, 0.1)):
+        decay[p:p + n] = d
+    check_step(s, before, states, 1, s.states(), decay=decay, lr=0.01)
+
+
+def test_states_in_8_bits_are_right_on_average():
+    """Constant gradients g: m tends to g, and v to g^2 (1 - beta2^t), where the nearest code would hold the root at a few steps' value. Over n values:
+
+    m: a rounding is right on average with a variance of at most (2^-3 m)^2 / 4; m remembers 1 / (1 - beta1^2) = 5.3 of them.
+    v: the root r is rounded right on average, so v gains the variance of r. A move of r by d between codes D apart has one of d * D at the most, with
+    d = r / (2t) and D <= r / 8 at step t: v / (16 t) = g^2 (1 - beta2) / 16 a step, one 16th of v's own growth, and on what was gained again: at most one 15th,
+    with one 14th for what is not linear in it. Its standard deviation is sqrt(sum of 4 v_t^2 / (16 t)) = 0.35 v."""
+    n, steps = 1 << 16, 300
+    g = torch.full((n,), 0.3, device="cuda") * (1 + torch.arange(n, device="cuda") % 7)
+    opt = tn.AdamW([torch.zeros(n, device="cuda")], lr=0.0, betas=(0.9, 0.999), state_bits=8, seed=5)
+    for _ in range(steps):
+        opt.step([g])
+    s = opt.state_dict()
+    value = lambda k: (s[k].float().view(-1, 128) * s[k + "_scales"].float()[:, None]).view(-1)      # noqa: E731
+    ratio_m = host(value("first") / g)
+    ratio_v = host(value("second") ** 2 / g ** 2) / (1 - 0.999 ** steps)
+    assert abs(ratio_m.mean() - 1) < 5 * 2.0 ** -4 * 5.3 ** 0.5 / n ** 0.5
+    assert -5 * 0.35 / n ** 0.5 < ratio_v.mean() - 1 < 1 / 14 + 5 * 0.35 / n ** 0.5
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_same_from_run_to_run_and_from_a_saved_state(bits):
+    a, b = (Setup(SIZES, "mixed", "mixed", bits, seed=2) for _ in range(2))
+    for _ in range(3):
+        a.opt.step(a.grads, max_norm=1.0)
+        b.opt.step(b.grads, max_norm=1.0)
+    again = tn.AdamW([p.clone() for p, _ in a.params], lr=LR, betas=BETAS, eps=EPS, weight_decay=DECAY, state_bits=bits, seed=77)
+    again.load_state_dict({k: v.clone() for k, v in a.opt.state_dict().items()})
+    for s in (a, b):
+        s.opt.step(s.grads)
+    again.step(a.grads)
+    for k, v in a.opt.state_dict().items():
+        raw = lambda t: t.view(torch.uint8) if t.dim() else t      # noqa: E731
+        assert torch.equal(raw(v), raw(b.opt.state_dict()[k])) and torch.equal(raw(v), raw(again.state_dict()[k])), k
+    for (p, _), (q, _), r in zip(a.params, b.params, again.params):
+        assert torch.equal(p, q) and torch.equal(p, r)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_captured_step(bits):
+    """A replayed step counts on, reads the gradients and the rate that are there, and gives what eager steps give."""
+    a, b = (Setup(SIZES + MANY[:300], "mixed", "f32", bits, seed=4) for _ in range(2))
+    rate = torch.tensor(LR, device="cuda")
+    a.opt.step(a.grads, lr=rate, max_norm=1.0)
+    b.opt.step(b.grads, lr=LR, max_norm=1.0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = a.opt.step(a.grads, lr=rate, max_norm=1.0)
+    for i in range(4):
+        for g, h in zip(a.grads, b.grads):
+            g.mul_(0.5)
+            h.mul_(0.5)
+        rate.fill_(LR * (i + 1))
+        graph.replay()
+        want = b.opt.step(b.grads, lr=float(torch.tensor(LR * (i + 1))), max_norm=1.0)
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want)
+        for k, v in a.opt.state_dict().items():
+            raw = lambda t: t.view(torch.uint8) if t.dim() else t      # noqa: E731
+            assert torch.equal(raw(v), raw(b.opt.state_dict()[k])), k
+        assert all(torch.equal(p, q) for (p, _), (q, _) in zip(a.params, b.params))
+
+
+def test_reset_master():
+    s = Setup([100, 50], "bf16", "f32", 32)
+    s.opt.step(s.grads)
+    s.params[0][0].fill_(0.5)
+    s.opt.reset_master()
+    assert bool((s.opt.state_dict()["master"][:100] == 0.5).all()) and int(s.opt.state_dict()["count"]) == 1
+    s.opt.step(s.grads)
+    s.check_around()
+
+
+def test_refusals():
+    p, q = torch.zeros(100, device="cuda"), torch.zeros(50, dtype=torch.bfloat16, device="cuda")
+    for bad in ([], [p, p], [p, p[50:60]], [p.half()], [p.cpu()], [p.view(10, 10).t()], [None]):
+        with pytest.raises(ValueError):
+            tn.AdamW(bad)
+    for more in (dict(lr=-1.0), dict(lr=float("nan")), dict(betas=(1.0, 0.9)), dict(betas=(0.9, -0.1)), dict(eps=-1e-8), dict(state_bits=16), dict(weight_decay=[0.1]),
+                 dict(weight_decay=-0.1), dict(seed=-1), dict(seed=1 << 32)):
+        with pytest.raises(ValueError):
+            tn.AdamW([p, q], **more)
+    opt = tn.AdamW([p, q])
+    g, h = torch.zeros(100, device="cuda"), torch.zeros(50, device="cuda")
+    for bad in ([g], [g, h, h], [g, None], [g.half(), h], [h, g], [g, h.cpu()], [torch.zeros(200, device="cuda")[::2], h]):
+        for call in (opt.step, opt.gradient_norm):
+            with pytest.raises(ValueError):
+                call(bad)
+    for more in (dict(lr=-1.0), dict(lr=float("inf")), dict(lr=torch.zeros(2, device="cuda")), dict(lr=torch.zeros((), dtype=torch.float64, device="cuda")), dict(max_norm=0.0),
+                 dict(max_norm=float("nan")), dict(norm=torch.zeros((), device="cuda")), dict(max_norm=1.0, norm=torch.zeros(()))):
+        with pytest.raises(ValueError):
+            opt.step([g, h], **more)
+    with pytest.raises(ValueError):
+        opt.load_state_dict({"first": p})
+    state = {k: v.clone() for k, v in opt.state_dict().items()}
+    with pytest.raises(ValueError):
+        opt.load_state_dict({**state, "first": state["first"][:-128]})
+    assert int(opt.state_dict()["count"]) == 0
+    opt.close()
+    with pytest.raises(RuntimeError):
+        opt.step([g, h])

@@ -1,0 +1,142 @@
+"""Projections with 4-bit weights, what needs no GPU: the oracle's own pins, the C ABI's refusals, the binding's checks, the choice of a kernel."""
+import ctypes
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import oracle.int4_oracle as I
+import paper_2602_01613_amd as tn
+from paper_2602_01613_amd import fp8, int4
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+INVALID, UNSUPPORTED = -1, -2
+A = 1 << 20
+
+
+def test_oracle_packs_and_dequantises():
+    rng = np.random.default_rng(0)
+    for n in (1, 2, 7, 130):
+        codes = rng.integers(0, 16, (5, n), dtype=np.uint8)
+        packed = I.pack(codes)
+        assert packed.shape == (5, (n + 1) // 2) and np.array_equal(I.unpack(packed, n), codes)
+        assert packed[0, 0] & 15 == codes[0, 0] and (n < 2 or packed[0, 0] >> 4 == codes[0, 1])
+    codes, scales = rng.integers(0, 16, (3, 70), dtype=np.uint8), rng.standard_normal((3, 3))
+    zeros = rng.integers(0, 16, (3, 3), dtype=np.uint8)
+    w = I.weight(codes, scales, zeros, 32)
+    for f in range(3):
+        for k in range(70):
+            assert w[f, k] == (int(codes[f, k]) - int(zeros[f, k // 32])) * scales[f, k // 32]
+    assert np.array_equal(I.weight(codes, scales, None, 32), I.weight(codes, scales, np.full((3, 3), 8), 32))
+
+
+def test_oracle_quantises_within_its_step():
+    rng = np.random.default_rng(1)
+    w = rng.standard_normal((40, 200)).astype(np.float32)
+    w[0], w[1], w[2] = 0, np.abs(w[1]), -np.abs(w[2])
+    codes, scales, zeros = I.quantize(w, 64)
+    assert codes.max() <= 15 and zeros.max() <= 15 and (codes[0] == 8).all() and (zeros[0] == 8).all() and (scales[0] == 0).all()
+    assert (zeros[1] == 0).all() and (zeros[2] == 15).all()
+    err = np.abs(I.weight(codes, scales, zeros, 64) - w)
+    assert (err <= (1 + 15 * 2.0 ** -8) * np.repeat(scales, 64, axis=1)[:, :200]).all()
+    assert np.array_equal(I.bf16(np.float32([1.00390625, 1.01171875])), np.float32([1.0, 1.015625]))          # ties to even
+
+
+def test_header_declares_what_the_binding_exports():
+    text = open(os.path.join(os.path.dirname(HERE), "include", "tn_int4.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    declared = set(re.findall(r"\b(tn_int4_[a-z_0-9]+)\s*\(", text))
+    assert declared == set(tn.INT4_EXPORTED_SYMBOLS)
+    lib = tn.load_library()
+    for name in declared:
+        assert hasattr(lib, name), name
+
+
+def _desc(**change):
+    d = int4._Desc()
+    fields = dict(dtype=3, n_tensors=1, out_features=10, in_features=10, group=32, scale_dtype=1, tensors=[A], scales=[A], zeros=None, flags=0, stream=None)
+    fields.update(change)
+    keep = []
+    for key in ("tensors", "scales", "zeros"):
+        if fields[key] is not None:
+            arr = (ctypes.c_void_p * len(fields[key]))(*fields[key])
+            keep.append(arr)
+            fields[key] = arr
+    for key, value in fields.items():
+        if value is not None:
+            setattr(d, key, value)
+    return d, keep
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=2), INVALID), (dict(dtype=-1), INVALID), (dict(n_tensors=0), INVALID), (dict(n_tensors=3, tensors=[A] * 3, scales=[A] * 3), INVALID),
+    (dict(out_features=0), INVALID), (dict(in_features=-4), INVALID), (dict(group=16), INVALID), (dict(group=256), INVALID), (dict(group=0), INVALID),
+    (dict(scale_dtype=0), INVALID), (dict(scale_dtype=2), INVALID), (dict(flags=2), INVALID), (dict(tensors=None), INVALID), (dict(tensors=[None]), INVALID),
+    (dict(scales=None), INVALID), (dict(scales=[None]), INVALID), (dict(scales=[A + 1]), INVALID), (dict(zeros=[None]), INVALID),
+    (dict(dtype=0, tensors=[A + 2]), INVALID), (dict(dtype=1, tensors=[A + 1]), INVALID), (dict(n_tensors=2, tensors=[A, None], scales=[A, A]), INVALID),
+    (dict(out_features=1 << 23), UNSUPPORTED), (dict(in_features=1 << 40), UNSUPPORTED)])
+def test_layer_descriptions_refused(change, status):
+    h = ctypes.c_void_p(0)
+    d, keep = _desc(**change)
+    assert int4._library().tn_int4_linear_create(ctypes.byref(h), ctypes.byref(d)) == status
+    assert not h.value
+
+
+def test_null_handles():
+    lib = int4._library()
+    d, keep = _desc()
+    value = ctypes.c_int64(0)
+    assert lib.tn_int4_linear_create(None, ctypes.byref(d)) == INVALID
+    assert lib.tn_int4_linear_create(ctypes.byref(ctypes.c_void_p(0)), None) == INVALID
+    assert lib.tn_int4_linear_workspace(None, A, 10, 1, 0) == INVALID
+    assert lib.tn_int4_linear_forward(None, A, 10, A, 10, 1, None, 0, None) == INVALID
+    assert lib.tn_int4_linear_gated(None, A, 10, A, 10, 1, None, 0, None) == INVALID
+    assert lib.tn_int4_linear_tensor(None, 0, A, A, A, None) == INVALID
+    assert lib.tn_int4_linear_query(None, tn.TN_QUERY_OUT_FEATURES, ctypes.byref(value)) == INVALID
+    assert lib.tn_int4_linear_destroy(None) == 0
+
+
+def test_plan_queries_refuse():
+    lib = int4._library()
+    value = ctypes.c_int64(0)
+    d, keep = _desc(tensors=None, n_tensors=2)
+    ask = lambda tokens=1, gated=0, what=0, desc=d: lib.tn_int4_linear_plan_query(ctypes.byref(desc) if desc else None, tokens, gated, what, ctypes.byref(value))      # noqa: E731
+    assert ask() == 0 and ask(gated=1) == 0
+    assert ask(tokens=0) == INVALID and ask(what=99) == INVALID and ask(desc=None) == INVALID and ask(tokens=1 << 40) == UNSUPPORTED
+    one, keep1 = _desc(tensors=None)
+    back, keep2 = _desc(tensors=None, n_tensors=2, flags=tn.TN_FLAG_TRANSPOSE)
+    assert ask(gated=1, desc=one) == INVALID and ask(gated=1, desc=back) == INVALID and ask(desc=back) == 0
+    assert lib.tn_int4_linear_plan_query(ctypes.byref(d), 1, 0, 0, None) == INVALID
+
+
+def test_binding_refuses(monkeypatch):
+    """Arguments that do not fit are refused before the library is reached."""
+    from fp8_util import on_gpu
+    monkeypatch.setattr(fp8, "_current_gpu", lambda: 0)
+    monkeypatch.setattr(int4, "_library", lambda: pytest.fail("reached the library"))
+    here = lambda shape, dtype, gpu=0: on_gpu(torch.zeros(shape, dtype=dtype), gpu)      # noqa: E731
+    codes, s, z = here((4, 5), torch.uint8), here((4, 1), torch.bfloat16), here((4, 1), torch.uint8)
+    ok = dict(tensors=[codes], max_tokens=1, transpose=False, group=128, scales=[s], zeros=[z], in_features=None)
+    int4._description(**ok)
+    int4._description(**{**ok, "in_features": 9})
+    int4._description(**{**ok, "tensors": [here((4, 10), torch.float32)], "scales": None, "zeros": None})
+    for change in (dict(tensors=[]), dict(tensors=[codes] * 3), dict(tensors=[codes, here((4, 6), torch.uint8)]), dict(max_tokens=0), dict(group=100), dict(scales=None),
+                   dict(scales=[s, s]), dict(scales=[here((4, 1), torch.float32)]), dict(scales=[here((4, 2), torch.bfloat16)]), dict(scales=[here((4, 1), torch.bfloat16, 1)]),
+                   dict(zeros=[here((4, 1), torch.int8)]), dict(zeros=[z, z]), dict(zeros=[here((3, 1), torch.uint8)]), dict(in_features=8), dict(in_features=11),
+                   dict(tensors=[here((4, 5), torch.uint8, 1)]), dict(tensors=[here((4, 5), torch.int8)]), dict(tensors=[torch.zeros((4, 5), dtype=torch.uint8)]),
+                   dict(tensors=[here((4, 10), torch.float32)]), dict(tensors=[here((4, 10), torch.float32)], scales=None, zeros=[z]),
+                   dict(tensors=[here((4, 10), torch.float32)], scales=None, zeros=None, in_features=9), dict(tensors=[here((4, 10), torch.float16)], scales=None, zeros=None),
+                   dict(tensors=[here((5, 4), torch.uint8).t()])):
+        with pytest.raises(ValueError):
+            int4._description(**{**ok, **change})
+    monkeypatch.setattr(fp8, "_current_gpu", lambda: 1)
+    with pytest.raises(ValueError):
+        int4._description(**ok)
+
+
+def test_needs_a_gpu():
+    if not torch.cuda.is_available():
+        with pytest.raises(RuntimeError):
+            tn.Int4Linear([torch.zeros(4, 4)], 1)
