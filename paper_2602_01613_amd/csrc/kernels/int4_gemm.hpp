@@ -4,10 +4,12 @@
 
 // ---------------------------------------------------------------------------------------------
 // A workgroup of four waves computes 16 * TM tokens x 256 features: each wave all of the tokens x 64 features, in TM x 4 accumulators of
-// v_mfma_f32_16x16x32_bf16. Side by side along the features, no two waves make the same weight: its codes go from memory to registers in the
-// operand's order (1 KB a load) and become bf16 there, 20 vector instructions for 512 weights, dealt out between the MFMAs of the step before.
-// The tokens go from memory to LDS without passing through registers, in three stages of 64 k; a row is 128 bytes there, its 16-byte chunk c at
-// position c ^ ((row / 2) % 8), so that the 16 rows a read touches at a time fall on 16 different slots of the 64 banks.
+// v_mfma_f32_16x16x32_f16. Side by side along the features, no two waves make the same weight: its codes go from memory to registers in the
+// operand's order (1 KB a load) and become fp16 there, (code - zero) * (scale / 2^e) with one rounding of 2^-12; two weights are a shift, a mask, an or, an addition
+// and a multiplication of packed halves, dealt out between the MFMAs of the step before. (In bf16 the rounding was 2^-9, as large as the output's, and the
+// conversion half as long again.) The tokens, in fp16 under a power of two for each row, go from memory to LDS without passing through registers, in three stages
+// of 64 k; a row is 128 bytes there, its 16-byte chunk c at position c ^ ((row / 2) % 8), so that the 16 rows a read touches at a time fall on 16
+// different slots of the 64 banks.
 //
 // A step is 32 k: 4 * TM MFMAs, tokens outermost. Behind the four of token fragment i the fragment that the next step has in its place is
 // read into the same registers. A stage is two steps; what the first one reads (its second half) are the last reads of the stage, so that after the
@@ -25,8 +27,18 @@ struct Int4GemmArgs {
 template <int TM>
 struct Int4Shape {
     static constexpr int BM = 16 * TM, STAGE = BM * 128, NS = 3, SMEM = NS * STAGE;
-    static constexpr int PER_CU = TM <= 8 ? 2 : 1;
+    static constexpr int PER_CU = TM <= 4 ? 2 : 1;
 };
+
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ floatx4 mfma16h(uintx4 w, halfx8 x, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, w), x, c, 0, 0, 0); }
+
+// Two weights from element pair `pair` of a word of codes: 1024 + code is a code in the low bits of an fp16 1024, and all up to the product exact
+__device__ __forceinline__ unsigned weights_as_half(unsigned w, int pair, halfx2 scale, halfx2 offset) {
+    const halfx2 h = __builtin_bit_cast(halfx2, ((w >> (4 * pair)) & 0x000F000Fu) | 0x64006400u);
+    return __builtin_bit_cast(unsigned, (h + offset) * scale);
+}
 
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
@@ -38,11 +50,23 @@ __device__ __forceinline__ void for_constants(F&& f, std::integer_sequence<int, 
 }
 
 #ifdef __HIP_DEVICE_COMPILE__
+// keeps accumulators where they are across a loop's back edge: in the accumulation registers where they are more than half of all
+template <int TM>
+__device__ __forceinline__ void pin(floatx4 (&acc)[TM][4]) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            if constexpr (TM >= 8) asm volatile("" : "+a"(acc[i][f]));
+            else asm volatile("" : "+v"(acc[i][f]));
+        }
+}
+
 template <int TM, int FORM, bool TRANSPOSED, int SUB>
 __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
     using S = Int4Shape<TM>;
     constexpr int LOADS = TM / 2;                 // of a stage, to a wave: 8 rows each
-    static_assert(TM % 4 == 0, "whole loads for each wave, reads behind the barrier");
+    static_assert(TM % 2 == 0, "whole loads for each wave");
     typedef __attribute__((address_space(3))) void lds_t;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const Int4Args& a = g.l;
@@ -65,7 +89,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
     constexpr int RSRC = 0x00020000;
     const int row_bytes = int(a.x_stride) * 2, rows = int(min(a.tokens - int64_t(row_tile) * S::BM, int64_t(S::BM)));
     const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<bf16_t*>(a.x + int64_t(row_tile) * S::BM * a.x_stride), 0, (rows - 1) * row_bytes + a.k_blocks * (kBlock * 2), RSRC);
+        const_cast<_Float16*>(static_cast<const _Float16*>(a.x) + int64_t(row_tile) * S::BM * a.x_stride), 0, (rows - 1) * row_bytes + a.k_blocks * (kBlock * 2), RSRC);
     const int vx = (wave * 8 + (lane >> 3)) * row_bytes + (((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))) * 16);
     const int last_stage = (kb0 + nk) * 2 - 1;
     auto load_x = [&](int n, int at, unsigned char* s) {              // n: load of the stage; at: stage in memory
@@ -85,8 +109,8 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
 #pragma unroll
     for (int f = 0; f < 4; ++f) {
         codes[f] = a.packed + int64_t(piece_of(f)) * a.k_blocks * kPieceWords + lane * 4;
-        words[f] = TRANSPOSED ? a.words + piece_of(f) / a.group_pieces * a.word_stride + (lane >> 4) * 8
-                              : a.words + int64_t(piece_of(f)) * a.k_blocks * (SUB * kPiece) + (lane & 15);
+        words[f] = TRANSPOSED ? a.halves + piece_of(f) / a.group_pieces * a.word_stride + (lane >> 4) * 8
+                              : a.halves + int64_t(piece_of(f)) * a.k_blocks * (SUB * kPiece) + (lane & 15);
     }
     // Transposed: scales along k, the same for the pieces of a group, of which the wave has SUB (1 for groups of 64 and more, 2 for 32)
     constexpr int NW = TRANSPOSED ? SUB : 4;
@@ -106,7 +130,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
                 for (int s = 0; s < SUB; ++s) w.w[f][s] = words[f][(int64_t(at) * SUB + s) * kPiece];
         }
     };
-    // transposed: the words of the lane's 8 k of a step
+    // transposed: scales and zeros of the lane's 8 k of a step
     uintx4 kw[NW][2];
     auto load_words = [&](int kb, int j) {
         const int at = min(kb, kb0 + nk - 1);
@@ -120,21 +144,20 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
 
     const int r = lane & 15, kq = lane >> 4;
     const int o0 = r * 128 + ((kq ^ (r >> 1)) * 16), o1 = r * 128 + (((4 + kq) ^ (r >> 1)) * 16);
-    bf16x8 fx[TM];
+    halfx8 fx[TM];
     uintx4 fw[2][4];
     floatx4 acc[TM][4];
-    auto read_x = [&](int i, int half, const unsigned char* s) { fx[i] = *reinterpret_cast<const bf16x8*>(s + (half ? o1 : o0) + i * 2048); };
+    auto read_x = [&](int i, int half, const unsigned char* s) { fx[i] = *reinterpret_cast<const halfx8*>(s + (half ? o1 : o0) + i * 2048); };
     // word `at` of the 16 (pair p of fragment f) of step j
     auto make = [&](uintx4 (&to)[4], const uintx4 (&c)[4], const Words& w, int j, int at) {
         const int f = at >> 2, p = at & 3;
         if constexpr (TRANSPOSED) {
             const int n = f / (4 / NW);
-            const unsigned w0 = kw[n][p >> 1][2 * (p & 1)], w1 = kw[n][p >> 1][2 * (p & 1) + 1];
-            to[f][p] = weights_as_bf16(c[f][j], p, word_scale(w0), word_offset(w0), word_scale(w1), word_offset(w1));
+            const unsigned scales = kw[n][0][p], offsets = kw[n][1][p];          // (a cast of the element itself takes the vector's first)
+            to[f][p] = weights_as_half(c[f][j], p, __builtin_bit_cast(halfx2, scales), __builtin_bit_cast(halfx2, offsets));
         } else {
-            const unsigned s = w.w[f][j * SUB / 4];
-            const float scale = word_scale(s), offset = word_offset(s);
-            to[f][p] = weights_as_bf16(c[f][j], p, scale, offset, scale, offset);
+            const halfx2 w2 = __builtin_bit_cast(halfx2, w.w[f][j * SUB / 4]);
+            to[f][p] = weights_as_half(c[f][j], p, halfx2{w2[0], w2[0]}, halfx2{w2[1], w2[1]});
         }
     };
 
@@ -148,6 +171,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int f = 0; f < 4; ++f) acc[i][f] = floatx4{0.f, 0.f, 0.f, 0.f};
+    pin(acc);
 #pragma unroll
     for (int at = 0; at < 16; ++at) make(fw[0], now, words_now, 0, at);
     load_words(kb0, 1);
@@ -164,7 +188,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
             unsigned char* s = smem + stage;
             const int after = stage == (S::NS - 1) * S::STAGE ? 0 : stage + S::STAGE;
             unsigned char* sn = smem + after;
-            constexpr int BAR = 2;                // second half: reads start behind the barrier, which is in front of this fragment
+            constexpr int BAR = TM > 2 ? 2 : 1;   // second half: reads start behind the barrier, which is in front of this fragment
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
@@ -178,13 +202,14 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
                 }
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
-                    acc[i][f] = mfma16(operand(fw[half][f]), fx[i], acc[i][f]);
+                    acc[i][f] = mfma16h(fw[half][f], fx[i], acc[i][f]);
                     const int slot = i * 4 + f;
-                    constexpr int EVERY = TM / 4;
-                    if (slot % EVERY == EVERY - 1) {
-                        if (j == 3) make(fw[0], next, words_next, 0, slot / EVERY);
-                        else make(fw[1 - half], now, words_now, j + 1, slot / EVERY);
-                    }
+#pragma unroll
+                    for (int at = 0; at < 16; ++at)              // the 16 words, dealt over the slots
+                        if ((TM < 4 ? at * TM / 4 : (at + 1) * TM / 4 - 1) == slot) {
+                            if (j == 3) make(fw[0], next, words_next, 0, at);
+                            else make(fw[1 - half], now, words_now, j + 1, at);
+                        }
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (!half) {
@@ -204,6 +229,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
             }
             if (TRANSPOSED) load_words(kb0 + kb + (j >= 2 ? 1 : 0), (j + 2) & 3);
             if (half) stage = after;
+            pin(acc);
         };
         step(std::integral_constant<int, 0>());
         step(std::integral_constant<int, 1>());
@@ -218,10 +244,18 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
 
     // lane: token l % 16 of fragment i, features 4 * (l / 16) .. + 3 of fragment f
     const int64_t row0 = int64_t(row_tile) * S::BM;
+    int exponents[4][4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) __builtin_memcpy(exponents[f], a.exponents + int64_t(piece_of(f)) * kPiece + kq * 4, 16);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int64_t token = row0 + i * 16 + r;
         if (token >= a.tokens) continue;
+        const int e = a.x_exponents[token];
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[i][f][q] = ldexpf(acc[i][f][q], exponents[f][q] + e);
         if constexpr (FORM == INT4_PARTIAL) {
             float* p = a.partial + (int64_t(split) * a.tokens + token) * a.ld + first * kPiece + kq * 4;
 #pragma unroll

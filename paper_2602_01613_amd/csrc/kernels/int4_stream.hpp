@@ -6,8 +6,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 
 struct Int4Args {
-    const bf16_t* x;                           // rows 16-byte aligned, whole blocks of k, zeros where there is no input
-    const unsigned *packed, *words;
+    const void* x;                             // rows 16-byte aligned, whole blocks of k, zeros where there is no input: bf16, for tiles fp16
+    const int32_t* x_exponents;                // tiles: of the rows
+    const unsigned *packed, *words, *halves;
+    const int32_t* exponents;                  // of the features, for tiles
     bf16_t* y;
     float* partial;                            // fp32 sums [n_split][tokens][ld] of padded features
     int64_t tokens, x_stride, y_stride, ld;
@@ -32,52 +34,24 @@ __device__ __forceinline__ bf16x8 codes_as_bf16(unsigned w) {
 }
 __device__ __forceinline__ float word_scale(unsigned s) { return __uint_as_float(s & ~15u); }
 __device__ __forceinline__ float sixteen_and_zero(unsigned s) { return __uint_as_float(0x41800000u | ((s & 15u) << 19)); }       // 16 + zero
-__device__ __forceinline__ float word_offset(unsigned s) { return -__uint_as_float(0x44800000u | ((s & 15u) << 13)) * word_scale(s); }  // -(1024 + zero) * scale, exact
-
-// Two weights in bf16 from element pair `pair` of a word: with the code in the mantissa of an fp16 1024 the product with the scale and the
-// offset -(1024 + zero) * scale are one fused operation that has nothing to round, (code - zero) * scale is at most 16 bits long.
-__device__ __forceinline__ unsigned weights_as_bf16(unsigned w, int pair, float s0, float c0, float s1, float c1) {
-    typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const halfx2 h = __builtin_bit_cast(halfx2, ((w >> (4 * pair)) & 0x000F000Fu) | 0x64006400u);
-    bf16x2 r;
-    r[0] = bf16_t(fmaf(float(h[0]), s0, c0));
-    r[1] = bf16_t(fmaf(float(h[1]), s1, c1));
-    return __builtin_bit_cast(unsigned, r);
-}
-
-// Four neighbouring outputs of a token by the definition, in fp32: for results that are not finite. (The sums of 16 + code lose an infinity's sign to
-// inf - inf, and may overflow where the weights' do not.)
-__device__ __noinline__ floatx4 plain_sums(const Int4Args& a, int64_t piece, int f0, int64_t token) {
-    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
-    const bf16_t* x = a.x + token * a.x_stride;
-    for (int kb = 0; kb < a.k_blocks; ++kb)
-        for (int at = 0; at < 16; ++at) {                                   // runs of 8 k
-            const int j = at >> 2, quarter = at & 3;
-            const bf16_t* p = x + kb * kBlock + at * 8;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const unsigned w = a.packed[(piece * a.k_blocks + kb) * kPieceWords + (quarter * 16 + f0 + i) * 4 + j];
-                for (int e = 0; e < 8; ++e) {
-                    const unsigned s = a.transpose ? a.words[piece / a.group_pieces * a.word_stride + kb * kBlock + at * 8 + e]
-                                                   : a.words[((piece * a.k_blocks + kb) * a.sub + (at * a.sub >> 4)) * kPiece + f0 + i];
-                    const float q = float(int(w >> element_bit(e) & 15u) - int(s & 15u));
-                    sum[i] += q * word_scale(s) * float(p[e]);
-                }
-            }
-        }
+// One output by the definition, in fp32: for results that are not finite. (The sums of 16 + code lose an infinity's sign to inf - inf, and may overflow
+// where the weights' do not.)
+__device__ __forceinline__ float plain_sum(const unsigned* packed, const unsigned* words, const bf16_t* x, int k_blocks, int sub_shift, int block_step) {
+    float sum = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < k_blocks * kBlock; ++k) {
+        const int kb = k >> 7, in = k & 127;
+        const unsigned w = packed[int64_t(kb) * kPieceWords + ((in >> 3) & 3) * 64 + (in >> 5)];
+        const unsigned s = words[kb * int64_t(block_step) + (in >> sub_shift) * kPiece];
+        sum += float(int(w >> element_bit(in & 7) & 15u) - int(s & 15u)) * word_scale(s) * float(x[k]);
+    }
     return sum;
 }
 
 // (up to the sign of the exponent's last values: relative error 2^-21, and finite for every finite gate)
 __device__ __forceinline__ float gated_value(float gate, float up) { return gate * sigmoid(gate) * up; }
 
-__device__ __forceinline__ bool all_finite(floatx4 v) {
-    bool fine = true;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) fine = fine && (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u;
-    return fine;
-}
+__device__ __forceinline__ bool is_finite(float v) { return (__float_as_uint(v) & 0x7fffffffu) < 0x7f800000u; }
 
 // four neighbouring values of a row as bf16, of which n exist
 __device__ __forceinline__ void store4(bf16_t* p, int n, floatx4 v) {
@@ -94,42 +68,42 @@ __device__ __forceinline__ void store4(bf16_t* p, int n, floatx4 v) {
 // ---------------------------------------------------------------------------------------------
 // Y[t][f] = sum over groups g of scale[f][g] * (sum over k in g of (16 + code[f][k]) X[t][k] - (16 + zero[f][g]) * sum over k in g of X[t][k])
 //
-// on v_mfma_f32_16x16x32_bf16 with the weight as the first operand, so that a lane of the result holds four consecutive features of one token. 16 + code is
-// exact in bf16 and costs one shift, one mask and one or for two codes; the sums of X over a group come from the same instruction with ones for
-// weights, once for all pieces. A workgroup takes GROUPS pieces (gated: half of them gate's, half up's) and TG x 16 tokens, and all of k, which its
-// waves deal out BLOCKS blocks at a time and add up through LDS in a fixed order.
-// Transposed, the scales run along k: weights are made in bf16 with their scale before they are multiplied.
+// on v_mfma_f32_16x16x32_bf16 with the tokens as the first operand, so that a lane of the result holds four tokens of one feature and needs one scale
+// word a group. 16 + code is exact in bf16 and costs one shift, one mask and one or for two codes; the sums of X over a group come from the same
+// instruction with ones for weights, once for all pieces. A workgroup takes GROUPS pieces (gated: half of them gate's, half up's) and TG x 16
+// tokens, and all of k, which its waves deal out block by block and add up through LDS in a fixed order. Each wave has RING blocks requested ahead.
 // ---------------------------------------------------------------------------------------------
-template <int GROUPS, int TG, int SUB, bool TRANSPOSED>
+template <int GROUPS, int TG, int SUB>
 struct StreamBlock {
     uintx4 codes[GROUPS];
-    uintx4 words[TRANSPOSED ? 8 : GROUPS * SUB];        // transposed: of the lane's 4 x 8 k
+    unsigned words[GROUPS][SUB];
     bf16x8 x[TG][4];
 };
+template <int TG>
+constexpr int kRing = TG == 4 ? 2 : TG == 2 ? 3 : 4;
 
-template <int GROUPS, int TG, int SUB, bool TRANSPOSED, bool GATED>
+template <int GROUPS, int TG, int SUB, bool GATED>
 __global__ void __launch_bounds__(512) int4_stream_kernel(Int4Args a) {
-    constexpr int BLOCKS = TG == 1 ? 4 : TG == 2 ? 2 : 1;
+    constexpr int RING = kRing<TG>;
     __shared__ floatx4 part[8][GROUPS][TG][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    const int64_t token0 = int64_t(blockIdx.y) * (16 * TG) + (lane & 15);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     // gated: the first half of the pieces are gate's, the others up's
     constexpr int OWN = GATED ? GROUPS / 2 : GROUPS;
     const int piece0 = blockIdx.x * OWN;
     auto piece_of = [&](int g) { return GATED && g >= OWN ? a.f_pieces + piece0 + g - OWN : piece0 + g; };
+    const int64_t token0 = int64_t(blockIdx.y) * (16 * TG);
     const bf16_t* x[TG];
 #pragma unroll
     for (int t = 0; t < TG; ++t) {
-        const int64_t token = token0 + t * 16;           // rows past the end repeat the last one and are not stored
-        x[t] = a.x + (token < a.tokens ? token : a.tokens - 1) * a.x_stride + (lane >> 4) * 8;
+        const int64_t token = token0 + t * 16 + (lane & 15);           // rows past the end repeat the last one and are not stored
+        x[t] = static_cast<const bf16_t*>(a.x) + (token < a.tokens ? token : a.tokens - 1) * a.x_stride + (lane >> 4) * 8;
     }
     const unsigned* codes[GROUPS];
     const unsigned* words[GROUPS];
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
         codes[g] = a.packed + int64_t(piece_of(g)) * a.k_blocks * kPieceWords + lane * 4;
-        words[g] = TRANSPOSED ? a.words + piece_of(g) / a.group_pieces * a.word_stride + (lane >> 4) * 8
-                              : a.words + int64_t(piece_of(g)) * a.k_blocks * (SUB * kPiece) + (lane >> 4) * 4;
+        words[g] = a.words + int64_t(piece_of(g)) * a.k_blocks * (SUB * kPiece) + (lane & 15);
     }
     floatx4 out[GROUPS][TG];
 #pragma unroll
@@ -138,117 +112,106 @@ __global__ void __launch_bounds__(512) int4_stream_kernel(Int4Args a) {
         for (int t = 0; t < TG; ++t) out[g][t] = floatx4{0.f, 0.f, 0.f, 0.f};
     const bf16x8 ones = operand(uintx4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 
-    typedef StreamBlock<GROUPS, TG, SUB, TRANSPOSED> Block;
+    typedef StreamBlock<GROUPS, TG, SUB> Block;
     auto load = [&](Block& b, int kb) {
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            b.codes[g] = *reinterpret_cast<const uintx4*>(codes[g] + int64_t(kb) * kPieceWords);
-            if constexpr (!TRANSPOSED) {
+        for (int g = 0; g < GROUPS; ++g) b.codes[g] = *reinterpret_cast<const uintx4*>(codes[g] + int64_t(kb) * kPieceWords);
 #pragma unroll
-                for (int s = 0; s < SUB; ++s) b.words[g * SUB + s] = *reinterpret_cast<const uintx4*>(words[g] + (int64_t(kb) * SUB + s) * kPiece);
-            }
-        }
-        if constexpr (TRANSPOSED) {                      // (the host gives a workgroup pieces of one group)
+        for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) b.words[2 * j + h] = *reinterpret_cast<const uintx4*>(words[0] + int64_t(kb) * kBlock + j * 32 + h * 4);
-        }
+            for (int s = 0; s < SUB; ++s) b.words[g][s] = words[g][(int64_t(kb) * SUB + s) * kPiece];
 #pragma unroll
         for (int t = 0; t < TG; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) b.x[t][j] = *reinterpret_cast<const bf16x8*>(x[t] + int64_t(kb) * kBlock + j * 32);
+        __builtin_amdgcn_sched_barrier(0);
     };
     auto multiply = [&](const Block& b) {
-        if constexpr (TRANSPOSED) {
+        constexpr int STEPS = 4 / SUB;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float s[8], c[8];
+        for (int s = 0; s < SUB; ++s) {
+            floatx4 sums[TG];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const unsigned w = b.words[2 * j + (e >> 2)][e & 3];
-                    s[e] = word_scale(w);
-                    c[e] = word_offset(w);
-                }
+            for (int t = 0; t < TG; ++t) {
+                sums[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) {
-                    uintx4 v;
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) v[p] = weights_as_bf16(b.codes[g][j], p, s[2 * p], c[2 * p], s[2 * p + 1], c[2 * p + 1]);
-#pragma unroll
-                    for (int t = 0; t < TG; ++t) out[g][t] = mfma16(operand(v), b.x[t][j], out[g][t]);
-                }
+                for (int j = 0; j < STEPS; ++j) sums[t] = mfma16(b.x[t][s * STEPS + j], ones, sums[t]);
             }
-        } else {
-            constexpr int STEPS = 4 / SUB;
 #pragma unroll
-            for (int s = 0; s < SUB; ++s) {
-                floatx4 sums[TG];
+            for (int g = 0; g < GROUPS; ++g) {
+                floatx4 acc[TG];
 #pragma unroll
-                for (int t = 0; t < TG; ++t) {
-                    sums[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < TG; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < STEPS; ++j) sums[t] = mfma16(ones, b.x[t][s * STEPS + j], sums[t]);
+                for (int j = 0; j < STEPS; ++j) {
+                    const bf16x8 w = codes_as_bf16(b.codes[g][s * STEPS + j]);
+#pragma unroll
+                    for (int t = 0; t < TG; ++t) acc[t] = mfma16(b.x[t][s * STEPS + j], w, acc[t]);
                 }
+                const float scale = word_scale(b.words[g][s]), centre = sixteen_and_zero(b.words[g][s]);
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) {
-                    floatx4 acc[TG];
+                for (int t = 0; t < TG; ++t)
 #pragma unroll
-                    for (int t = 0; t < TG; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int j = 0; j < STEPS; ++j) {
-                        const bf16x8 w = codes_as_bf16(b.codes[g][s * STEPS + j]);
-#pragma unroll
-                        for (int t = 0; t < TG; ++t) acc[t] = mfma16(w, b.x[t][s * STEPS + j], acc[t]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const unsigned w = b.words[g * SUB + s][i];
-                        const float scale = word_scale(w), centre = sixteen_and_zero(w);
-#pragma unroll
-                        for (int t = 0; t < TG; ++t) out[g][t][i] = fmaf(scale, fmaf(-centre, sums[t][i], acc[t][i]), out[g][t][i]);
-                    }
-                }
+                    for (int i = 0; i < 4; ++i) out[g][t][i] = fmaf(scale, fmaf(-centre, sums[t][i], acc[t][i]), out[g][t][i]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    for (int kb = wave * BLOCKS; kb < a.k_blocks; kb += waves * BLOCKS) {
-        if (kb + BLOCKS <= a.k_blocks) {
-            Block b[BLOCKS];
+    // A ring of blocks, each requested again as soon as it has been multiplied; past the last one that one again, which is in the caches (a branch
+    // in the place of a load would make the waits for those before it wait for all).
+    const int n = a.k_blocks > wave ? (a.k_blocks - wave + waves - 1) / waves : 0;          // of this wave: wave, wave + waves, ...
+    if (n > 0) {
+        const int last = wave + (n - 1) * waves;
+        Block ring[RING];
 #pragma unroll
-            for (int q = 0; q < BLOCKS; ++q) load(b[q], kb + q);
+        for (int q = 0; q < RING; ++q) load(ring[q], min(wave + q * waves, last));
+        int i = 0;
+        for (; i + RING < n; i += RING) {
 #pragma unroll
-            for (int q = 0; q < BLOCKS; ++q) multiply(b[q]);
-        } else {
-            for (int q = kb; q < a.k_blocks; ++q) {
-                Block b;
-                load(b, q);
-                multiply(b);
+            for (int q = 0; q < RING; ++q) {
+                multiply(ring[q]);
+                load(ring[q], min(wave + (i + q + RING) * waves, last));
             }
         }
+#pragma unroll
+        for (int q = 0; q < RING; ++q)
+            if (i + q < n) multiply(ring[q]);
     }
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
         for (int t = 0; t < TG; ++t) part[wave][g][t][lane] = out[g][t];
     __syncthreads();
+    // lane: feature l % 16 of piece g, tokens 4 * (l / 16) .. + 3 of the 16
     auto total = [&](int g, int t, int64_t token) {
         floatx4 v = part[0][g][t][lane];
         for (int q = 1; q < waves; ++q) v += part[q][g][t][lane];
-        if (!all_finite(v)) v = plain_sums(a, piece_of(g), (lane >> 4) * 4, token);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (is_finite(v[i]) || token + i >= a.tokens) continue;
+            const int64_t piece = piece_of(g);
+            const int f = lane & 15;
+            const unsigned* p = a.packed + piece * a.k_blocks * kPieceWords + f * 4;
+            const bf16_t* row = static_cast<const bf16_t*>(a.x) + (token + i) * a.x_stride;
+            v[i] = plain_sum(p, a.words + piece * a.k_blocks * (SUB * kPiece) + f, row, a.k_blocks, SUB == 1 ? 7 : SUB == 2 ? 6 : 5, SUB * kPiece);
+        }
         return v;
     };
-    for (int i = wave; i < OWN * TG; i += waves) {
-        const int g = i / TG, t = i - g * TG;
-        const int64_t token = token0 + t * 16;
+    for (int u = wave; u < OWN * TG; u += waves) {
+        const int g = u / TG, t = u - g * TG;
+        const int64_t token = token0 + t * 16 + (lane >> 4) * 4;
         if (token >= a.tokens) continue;
         floatx4 v = total(g, t, token);
         if constexpr (GATED) {
             const floatx4 up = total(OWN + g, t, token);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[q] = gated_value(v[q], up[q]);
+            for (int i = 0; i < 4; ++i) v[i] = gated_value(v[i], up[i]);
         }
-        const int piece = piece0 + g, tensor = piece / a.f_pieces, f = (piece - tensor * a.f_pieces) * kPiece + (lane >> 4) * 4;
-        if (f < a.features) store4(a.y + token * a.y_stride + int64_t(tensor) * a.features + f, a.features - f, v);
+        const int piece = piece0 + g, tensor = piece / a.f_pieces, f = (piece - tensor * a.f_pieces) * kPiece + (lane & 15);
+        if (f >= a.features) continue;
+        bf16_t* y = a.y + token * a.y_stride + int64_t(tensor) * a.features + f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (token + i < a.tokens) y[i * a.y_stride] = bf16_t(v[i]);
     }
 }

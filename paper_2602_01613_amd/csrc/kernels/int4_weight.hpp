@@ -12,13 +12,18 @@
 // the low four. Of a tensor as it is, words lie [piece][k / 128][group within the 128][feature within the piece]; of a transposed one, whose
 // groups run along the features, [feature / group][k]. Features are padded to a multiple of 64 per tensor and k to one of 128 per
 // segment, with words of scale 0.
+//
+// Tiles multiply in fp16, for which there is a second word to a group: scale / 2^e in fp16 and -(1024 + zero), with e of the feature (transposed: of the group of
+// features) such that the largest of its scales is in [2^10, 2^11). A weight is at most 15 of them, and scales down to 2^-25 of the largest keep all
+// their bits. They lie like the others, but transposed the scales and the zeros of 8 k beside each other: [feature / group][k / 8][2][8] halves.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPiece = 16, kPieceWords = 256, kFeaturePad = 64;
 
 struct OperandArgs {
     const unsigned char *codes, *zeros;            // the tensor: [m][(n + 1) / 2], [m][groups]
     const void* scales;
-    unsigned *packed, *words;                      // the operand
+    unsigned *packed, *words, *halves;             // the operand
+    int32_t* exponents;                            // of its features
     int64_t m, n, groups;
     int32_t group, scale_f16, transpose;
     int32_t k_blocks, sub;                         // of the operand: blocks of 128 k, groups in one
@@ -60,6 +65,42 @@ __global__ void __launch_bounds__(256) int4_words_kernel(OperandArgs a) {
     } else {                                        // [piece][k / 128][group within][feature within]
         const int64_t per_piece = a.own_k_blocks * a.sub * kPiece, piece = i / per_piece, in = i - piece * per_piece;
         if (piece < a.f_pieces) a.words[(a.piece0 + piece) * per_piece + in] = scale_word(a, piece * kPiece + (in & 15), in >> 4);
+    }
+}
+
+// The least e for which |scale| < 2^(e + 11); 0 for no finite scale but zeros
+__device__ __forceinline__ int scale_exponent(unsigned most) { return most ? int(most >> 23) - 127 - 10 : 0; }
+__device__ __forceinline__ unsigned half_bits(float v) { return __builtin_bit_cast(unsigned short, _Float16(v)); }
+__device__ __forceinline__ unsigned half_word(unsigned word, int e) {                   // scale in the low half, -(1024 + zero) in the high one
+    return half_bits(ldexpf(__uint_as_float(word & ~15u), -e)) | half_bits(-1024.f - float(word & 15u)) << 16;
+}
+
+// The second words, from the first: a wave takes a feature of this tensor, or transposed (all tensors' k at once) a group of features
+__global__ void __launch_bounds__(256) int4_halves_kernel(OperandArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= (a.transpose ? (a.f_pieces * kPiece + a.group - 1) / a.group : a.f_pieces * kPiece)) return;
+    const int64_t count = a.transpose ? a.word_stride : a.own_k_blocks * a.sub;
+    const int64_t first = a.transpose ? row * a.word_stride : (a.piece0 + (row >> 4)) * count * kPiece + (row & 15), step = a.transpose ? 1 : kPiece;
+    unsigned most = 0;
+    for (int64_t i = lane; i < count; i += 64) most = max(most, finite_magnitude(__uint_as_float(a.words[first + i * step] & ~15u)));
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) most = max(most, unsigned(__shfl_xor(int(most), d)));
+    const int e = scale_exponent(most);
+    for (int64_t i = lane; i < count; i += 64) {
+        const unsigned w = half_word(a.words[first + i * step], e);
+        if (a.transpose) {
+            unsigned short* to = reinterpret_cast<unsigned short*>(a.halves) + row * a.word_stride * 2 + (i >> 3) * 16 + (i & 7);
+            to[0] = static_cast<unsigned short>(w);
+            to[8] = static_cast<unsigned short>(w >> 16);
+        } else {
+            a.halves[first + i * step] = w;
+        }
+    }
+    if (a.transpose) {
+        for (int64_t f = row * a.group + lane; f < min((row + 1) * a.group, a.f_pieces * kPiece); f += 64) a.exponents[f] = e;
+    } else if (lane == 0) {
+        a.exponents[a.piece0 * kPiece + row] = e;
     }
 }
 
@@ -130,4 +171,60 @@ __global__ void __launch_bounds__(256) int4_rows_kernel(const bf16_t* x, int64_t
         const Chunk<bf16_t> c = load_chunk(x + token * x_stride + segment * cols + (n ? k : 0), n);
         __builtin_memcpy(out + token * segments * padded + at, &c, sizeof(c));
     }
+}
+
+// The same rows in fp16 for the tiles, each divided by the power of two that puts its largest finite magnitude into [2^14, 2^15): exact but below 2^-29 of
+// that, and there off by 2^-40 of it at most. A workgroup takes a row; NC chunks of it stay in a thread's registers between the maximum and
+// the conversion, longer rows are read again from the caches.
+template <int NC>
+__global__ void __launch_bounds__(256) int4_half_rows_kernel(const bf16_t* x, int64_t x_stride, int32_t segments, int64_t cols, int64_t padded, _Float16* out,
+                                                             int32_t* exponents) {
+    __shared__ unsigned part[4];
+    const int64_t token = blockIdx.x, chunks = segments * padded / kChunk;
+    x += token * x_stride;
+    out += token * segments * padded;
+    auto load = [&](int64_t i) {
+        const int64_t at = i * kChunk, segment = segments == 1 ? 0 : at / padded, k = at - segment * padded, left = cols - k;
+        const int n = int(left < 0 ? 0 : left < kChunk ? left : kChunk);
+        return load_chunk(x + segment * cols + (n ? k : 0), n);
+    };
+    unsigned most = 0;
+    auto look = [&](const Chunk<bf16_t>& c) {
+#pragma unroll
+        for (int q = 0; q < kChunk; ++q) most = max(most, finite_magnitude(c[q]));
+    };
+    Chunk<bf16_t> held[NC];
+#pragma unroll
+    for (int h = 0; h < NC; ++h) {
+        const int64_t i = h * 256 + int(threadIdx.x);
+        if (i < chunks) held[h] = load(i);
+    }
+#pragma unroll
+    for (int h = 0; h < NC; ++h)
+        if (h * 256 + int(threadIdx.x) < chunks) look(held[h]);
+    for (int64_t i = NC * 256 + threadIdx.x; i < chunks; i += 256) look(load(i));
+    most = row16_max(most);
+    most = max(most, unsigned(__shfl_xor(int(most), 16)));
+    most = max(most, unsigned(__shfl_xor(int(most), 32)));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+    __syncthreads();
+    most = max(max(part[0], part[1]), max(part[2], part[3]));
+    // (bf16's subnormals have the exponent field 0: as if they were 2^-127, which keeps them in range)
+    const int e = most ? int(most >> 23) - 127 - 14 : 0;
+    auto store = [&](const Chunk<bf16_t>& c, int64_t i) {
+        uint4 w;
+        unsigned* p = &w.x;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+            const halfx2 h = {_Float16(ldexpf(c[2 * q], -e)), _Float16(ldexpf(c[2 * q + 1], -e))};
+            p[q] = __builtin_bit_cast(unsigned, h);
+        }
+        *reinterpret_cast<uint4*>(out + i * kChunk) = w;
+    };
+#pragma unroll
+    for (int h = 0; h < NC; ++h)
+        if (h * 256 + int(threadIdx.x) < chunks) store(held[h], h * 256 + int(threadIdx.x));
+    for (int64_t i = NC * 256 + threadIdx.x; i < chunks; i += 256) store(load(i), i);
+    if (threadIdx.x == 0) exponents[token] = e;
 }

@@ -36,11 +36,14 @@ struct tn_int4_linear_s {
     int32_t out_segments = 1, k_segments = 1;
     int64_t k_cols = 0;                   // inputs: segments of k_cols
     int64_t f_pieces = 0, own_k_blocks = 0, k_blocks = 0;
-    unsigned *packed = nullptr, *words = nullptr;
-    int64_t packed_bytes = 0, word_bytes = 0, word_stride = 0;
+    unsigned *packed = nullptr, *words = nullptr, *halves = nullptr;
+    int32_t* exponents = nullptr;
+    int64_t packed_bytes = 0, word_bytes = 0, word_stride = 0, exponent_bytes = 0;
     ~tn_int4_linear_s() {
         if (packed) (void)hipFree(packed);
         if (words) (void)hipFree(words);
+        if (halves) (void)hipFree(halves);
+        if (exponents) (void)hipFree(exponents);
     }
 };
 
@@ -69,6 +72,7 @@ void lay_out(const tn_int4_linear_desc& d, tn_int4_linear_s& h) {
     h.own_k_blocks = div_up(h.k_cols, kBlock);
     h.k_blocks = h.k_segments * h.own_k_blocks;
     h.packed_bytes = h.out_segments * h.f_pieces * h.k_blocks * kPieceWords * 4;
+    h.exponent_bytes = h.out_segments * h.f_pieces * kPiece * 4;
     h.word_stride = h.k_blocks * kBlock;
     h.word_bytes = 4 * (h.transpose ? div_up(h.f_pieces * kPiece, h.group) * h.word_stride
                                     : h.out_segments * h.f_pieces * h.k_blocks * (kBlock / h.group) * kPiece);
@@ -78,6 +82,8 @@ OperandArgs operand_args(const tn_int4_linear_s& h, int slot) {
     OperandArgs a{};
     a.packed = h.packed;
     a.words = h.words;
+    a.halves = h.halves;
+    a.exponents = h.exponents;
     a.m = h.m;
     a.n = h.n;
     a.groups = h.groups;
@@ -95,10 +101,12 @@ OperandArgs operand_args(const tn_int4_linear_s& h, int slot) {
 
 Int4Args product_args(const tn_int4_linear_s& h, const void* x, int64_t x_stride, int64_t tokens) {
     Int4Args a{};
-    a.x = static_cast<const bf16_t*>(x);
+    a.x = x;
     a.x_stride = x_stride;
     a.packed = h.packed;
     a.words = h.words;
+    a.halves = h.halves;
+    a.exponents = h.exponents;
     a.tokens = tokens;
     a.word_stride = h.word_stride;
     a.k_blocks = int32_t(h.k_blocks);
@@ -117,7 +125,7 @@ Int4Args product_args(const tn_int4_linear_s& h, const void* x, int64_t x_stride
 // which kernel a product runs on
 // ---------------------------------------------------------------------------------------------
 constexpr int64_t kStreamTokens = 64;           // streamed up to here
-constexpr int kTileTokens[] = {4, 8, 16};       // TM
+constexpr int kTileTokens[] = {2, 4, 8, 12};       // TM
 
 struct Choice {
     int tm = 0;                // tile of 16 * tm tokens; 0: streamed
@@ -128,7 +136,7 @@ struct Choice {
 Choice choose(const Int4Args& a, bool gated) {
     Choice c;
     const int64_t pieces = int64_t(a.f_pieces) * a.tensors;
-    if (a.tokens <= kStreamTokens) {
+    if (a.tokens <= kStreamTokens && !a.transpose) {
         c.tg = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
         return c;
     }
@@ -139,8 +147,8 @@ Choice choose(const Int4Args& a, bool gated) {
         for (const int split : {1, 2, 3, 4, 6, 8}) {
             if (split > 1 && split * 4 > a.k_blocks) break;
             const int64_t blocks = div_up(a.k_blocks, split), items = n_row * n_col * div_up(a.k_blocks, blocks);
-            const int per_cu = tm <= 8 ? 2 : 1;
-            const double k_block = tm == 4 ? 0.62 : tm == 8 ? 1.15 : 2.0;          // us of a workgroup, with per_cu on a CU
+            const int per_cu = tm <= 4 ? 2 : 1;
+            const double k_block = tm == 2 ? 0.4 : tm == 4 ? 0.62 : tm == 8 ? 1.0 : 1.4;          // us of a workgroup, with per_cu on a CU
             double us = div_up(items, kCUs * per_cu) * (blocks * k_block + 3.0);
             if (split > 1) us += 4.0 + double(a.tokens) * a.ld * 4 * 2 * split / 5e6;
             if (us < best) {
@@ -154,28 +162,26 @@ Choice choose(const Int4Args& a, bool gated) {
 }
 
 // Waves of a workgroup of the stream kernel: the number up to 8 that leaves the fewest of them idle in the last round
-int stream_waves(int k_blocks, int blocks) {
-    const int rounds = int(div_up(k_blocks, blocks));
+int stream_waves(int rounds) {
     int best = rounds < 8 ? rounds : 8;
     for (int w = best - 1; w >= 4; --w)
         if (div_up(rounds, w) * w < div_up(rounds, best) * best) best = w;
     return best;
 }
 
-template <int GROUPS, int TG, int SUB, bool TRANSPOSED, bool GATED>
+template <int GROUPS, int TG, int SUB, bool GATED>
 int run_stream(const Int4Args& a, hipStream_t stream) {
-    constexpr int OWN = GATED ? GROUPS / 2 : GROUPS, BLOCKS = TG == 1 ? 4 : TG == 2 ? 2 : 1;
+    constexpr int OWN = GATED ? GROUPS / 2 : GROUPS;
     const dim3 grid(unsigned((GATED ? a.f_pieces : int64_t(a.f_pieces) * a.tensors) / OWN), unsigned(div_up(a.tokens, 16 * TG)));
-    int4_stream_kernel<GROUPS, TG, SUB, TRANSPOSED, GATED><<<grid, dim3(64 * stream_waves(a.k_blocks, BLOCKS)), 0, stream>>>(a);
+    int4_stream_kernel<GROUPS, TG, SUB, GATED><<<grid, dim3(64 * stream_waves(a.k_blocks)), 0, stream>>>(a);
     return launched();
 }
 template <int GROUPS, int TG>
 int stream_form(const Int4Args& a, bool gated, hipStream_t stream) {
-    if (a.transpose) return run_stream<GROUPS, TG, 1, true, false>(a, stream);
     switch (a.sub) {
-        case 1: return gated ? run_stream<GROUPS, TG, 1, false, true>(a, stream) : run_stream<GROUPS, TG, 1, false, false>(a, stream);
-        case 2: return gated ? run_stream<GROUPS, TG, 2, false, true>(a, stream) : run_stream<GROUPS, TG, 2, false, false>(a, stream);
-        default: return gated ? run_stream<GROUPS, TG, 4, false, true>(a, stream) : run_stream<GROUPS, TG, 4, false, false>(a, stream);
+        case 1: return gated ? run_stream<GROUPS, TG, 1, true>(a, stream) : run_stream<GROUPS, TG, 1, false>(a, stream);
+        case 2: return gated ? run_stream<GROUPS, TG, 2, true>(a, stream) : run_stream<GROUPS, TG, 2, false>(a, stream);
+        default: return gated ? run_stream<GROUPS, TG, 4, true>(a, stream) : run_stream<GROUPS, TG, 4, false>(a, stream);
     }
 }
 
@@ -227,20 +233,36 @@ bool allow_tiles() {
            allow<TM, INT4_GATED, false, 1>() && allow<TM, INT4_GATED, false, 2>() && allow<TM, INT4_GATED, false, 4>();
 }
 
-// Rows that the products cannot read where they are
+// Rows that the streaming kernel cannot read where they are
 bool laid_out_anew(const tn_int4_linear_s& h, const void* x, int64_t x_stride) {
     return h.k_cols % kBlock != 0 || !aligned(x, 16) || x_stride % kChunk != 0 || x_stride >= kMaxStride;
 }
 struct Workspace {
-    int64_t rows = 0, sums = 0;
+    int64_t rows = 0, exponents = 0, sums = 0;
+    int64_t all() const { return rows + exponents + sums; }
 };
-Workspace workspace_of(const tn_int4_linear_s& h, const void* x, int64_t x_stride, int64_t tokens, bool gated) {
+Workspace workspace_of(const tn_int4_linear_s& h, const Int4Args& a, const Choice& c) {
     Workspace w;
-    if (laid_out_anew(h, x, x_stride)) w.rows = whole(tokens * h.k_blocks * kBlock * 2);
-    const Int4Args a = product_args(h, x, x_stride, tokens);
-    const Choice c = choose(a, gated);
-    if (c.tm && c.split > 1) w.sums = whole(c.split * tokens * a.ld * 4);
+    if (c.tm || laid_out_anew(h, a.x, a.x_stride)) w.rows = whole(a.tokens * h.k_blocks * kBlock * 2);
+    if (c.tm) w.exponents = whole(a.tokens * 4);
+    if (c.tm && c.split > 1) w.sums = whole(c.split * a.tokens * a.ld * 4);
     return w;
+}
+
+int half_rows(const tn_int4_linear_s& h, const Int4Args& a, _Float16* rows, int32_t* exponents, hipStream_t stream) {
+    const bf16_t* x = static_cast<const bf16_t*>(a.x);
+    const int64_t padded = h.own_k_blocks * kBlock, chunks = h.k_blocks * (kBlock / kChunk), run = int64_t(1) << 22;
+    for (int64_t at = 0; at < a.tokens; at += run) {              // a launch has fewer than 2^32 threads
+        const dim3 grid(unsigned(a.tokens - at < run ? a.tokens - at : run));
+        const bf16_t* from = x + at * a.x_stride;
+        _Float16* to = rows + at * h.k_blocks * kBlock;
+        if (chunks <= 512) int4_half_rows_kernel<2><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, to, exponents + at);
+        else if (chunks <= 1024) int4_half_rows_kernel<4><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, to, exponents + at);
+        else int4_half_rows_kernel<13><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, to, exponents + at);
+        const int rc = launched();
+        if (rc != TN_OK) return rc;
+    }
+    return TN_OK;
 }
 
 int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t tokens, bool gated, void* workspace,
@@ -252,26 +274,37 @@ int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void
     if (!x || !y || x_stride < x_cols || y_stride < y_cols || !aligned(x, 2) || !aligned(y, 2)) return TN_ERR_INVALID_ARG;
     // workgroups read rows of x while others write theirs of y
     if (overlap(x, ((tokens - 1) * x_stride + x_cols) * 2, y, ((tokens - 1) * y_stride + y_cols) * 2)) return TN_ERR_INVALID_ARG;
-    const Workspace w = workspace_of(h, x, x_stride, tokens, gated);
-    if (w.rows + w.sums > 0 && (!workspace || workspace_bytes < w.rows + w.sums || !aligned(workspace, 256))) return TN_ERR_INVALID_ARG;
-    if (w.rows) {
-        bf16_t* rows = static_cast<bf16_t*>(workspace);
-        const int64_t blocks = div_up(tokens * h.k_blocks * (kBlock / kChunk), 256);
-        int4_rows_kernel<<<dim3(unsigned(blocks < 32 * kCUs ? blocks : 32 * kCUs)), dim3(256), 0, stream>>>(
-            static_cast<const bf16_t*>(x), x_stride, tokens, h.k_segments, h.k_cols, h.own_k_blocks * kBlock, rows);
-        const int rc = launched();
-        if (rc != TN_OK) return rc;
-        x = rows;
-        x_stride = h.k_blocks * kBlock;
-    }
     Int4Args a = product_args(h, x, x_stride, tokens);
+    const Choice c = choose(a, gated);
+    const Workspace w = workspace_of(h, a, c);
+    if (w.all() > 0 && (!workspace || workspace_bytes < w.all() || !aligned(workspace, 256))) return TN_ERR_INVALID_ARG;
     a.y = static_cast<bf16_t*>(y);
     a.y_stride = y_stride;
-    const Choice c = choose(a, gated);
+    if (w.rows) {
+        int rc;
+        if (c.tm) {
+            int32_t* exponents = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + w.rows);
+            rc = half_rows(h, a, static_cast<_Float16*>(workspace), exponents, stream);
+            a.x_exponents = exponents;
+        } else {
+            const int64_t blocks = div_up(tokens * h.k_blocks * (kBlock / kChunk), 256);
+            int4_rows_kernel<<<dim3(unsigned(blocks < 32 * kCUs ? blocks : 32 * kCUs)), dim3(256), 0, stream>>>(
+                static_cast<const bf16_t*>(x), x_stride, tokens, h.k_segments, h.k_cols, h.own_k_blocks * kBlock, static_cast<bf16_t*>(workspace));
+            rc = launched();
+        }
+        if (rc != TN_OK) return rc;
+        a.x = workspace;
+        a.x_stride = h.k_blocks * kBlock;
+    }
     if (c.tm == 0) return c.tg == 1 ? stream_form<2, 1>(a, gated, stream) : c.tg == 2 ? stream_form<2, 2>(a, gated, stream) : stream_form<2, 4>(a, gated, stream);
     a.n_split = c.split;
-    if (c.split > 1) a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.rows);
-    return c.tm == 4 ? run_tiles<4>(a, gated, stream) : c.tm == 8 ? run_tiles<8>(a, gated, stream) : run_tiles<16>(a, gated, stream);
+    if (c.split > 1) a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.rows + w.exponents);
+    switch (c.tm) {
+        case 2: return run_tiles<2>(a, gated, stream);
+        case 4: return run_tiles<4>(a, gated, stream);
+        case 8: return run_tiles<8>(a, gated, stream);
+        default: return run_tiles<12>(a, gated, stream);
+    }
 }
 
 }  // namespace
@@ -293,12 +326,14 @@ int tn_int4_linear_create(tn_int4_linear_t* out, const tn_int4_linear_desc* d) {
     lay_out(*d, *h);
     const hipStream_t st = static_cast<hipStream_t>(d->stream);
     const int64_t row_bytes = div_up(h->n, 2);
-    int rc = allow_tiles<4>() && allow_tiles<8>() && allow_tiles<16>() ? TN_OK : TN_ERR_HIP;
+    int rc = allow_tiles<2>() && allow_tiles<4>() && allow_tiles<8>() && allow_tiles<12>() ? TN_OK : TN_ERR_HIP;
     // (what is quantised here passes through the form that a caller gives)
     unsigned char* made = nullptr;
     const int64_t scales_at = whole(h->m * row_bytes), zeros_at = scales_at + whole(h->m * h->groups * 2);
     if (rc == TN_OK && (hipMalloc(reinterpret_cast<void**>(&h->packed), size_t(h->packed_bytes)) != hipSuccess ||
                         hipMalloc(reinterpret_cast<void**>(&h->words), size_t(h->word_bytes)) != hipSuccess ||
+                        hipMalloc(reinterpret_cast<void**>(&h->halves), size_t(h->word_bytes)) != hipSuccess ||
+                        hipMalloc(reinterpret_cast<void**>(&h->exponents), size_t(h->exponent_bytes)) != hipSuccess ||
                         (!given && hipMalloc(reinterpret_cast<void**>(&made), size_t(zeros_at + h->m * h->groups)) != hipSuccess))) {
         (void)hipGetLastError();
         rc = TN_ERR_ALLOC;
@@ -325,6 +360,10 @@ int tn_int4_linear_create(tn_int4_linear_t* out, const tn_int4_linear_desc* d) {
         const int64_t words = h->transpose ? div_up(h->f_pieces * kPiece, h->group) * h->own_k_blocks * kBlock
                                            : h->f_pieces * h->own_k_blocks * a.sub * kPiece;
         int4_words_kernel<<<dim3(unsigned(div_up(words, 256))), dim3(256), 0, st>>>(a);
+        if (!h->transpose || i + 1 == h->tensors) {          // (transposed, a group of features has the scales of all tensors)
+            const int64_t waves = h->transpose ? div_up(h->f_pieces * kPiece, h->group) : h->f_pieces * kPiece;
+            int4_halves_kernel<<<dim3(unsigned(div_up(waves, 4))), dim3(256), 0, st>>>(a);
+        }
         rc = launched();
     }
     if (rc == TN_OK && hipStreamSynchronize(st) != hipSuccess) rc = TN_ERR_HIP;
@@ -344,8 +383,8 @@ int64_t tn_int4_linear_workspace(tn_int4_linear_t h, const void* x, int64_t x_st
     if (!h || tokens < 0 || (gated && h->out_segments != 2)) return TN_ERR_INVALID_ARG;
     if (tokens > kMaxRows) return TN_ERR_UNSUPPORTED;
     if (tokens == 0) return 0;
-    const Workspace w = workspace_of(*h, x, x_stride, tokens, gated != 0);
-    return w.rows + w.sums;
+    const Int4Args a = product_args(*h, x, x_stride, tokens);
+    return workspace_of(*h, a, choose(a, gated != 0)).all();
 }
 
 int tn_int4_linear_forward(tn_int4_linear_t h, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t tokens, void* workspace,
@@ -392,7 +431,7 @@ int tn_int4_linear_query(tn_int4_linear_t h, int32_t what, int64_t* value) {
         case TN_QUERY_OUT_FEATURES: *value = int64_t(h->out_segments) * h->features; return TN_OK;
         case TN_QUERY_IN_FEATURES: *value = h->k_segments * h->k_cols; return TN_OK;
         case TN_QUERY_PARAM_COUNT: *value = h->tensors * h->m * h->n; return TN_OK;
-        case TN_QUERY_PACKED_BYTES: *value = h->packed_bytes + h->word_bytes; return TN_OK;
+        case TN_QUERY_PACKED_BYTES: *value = h->packed_bytes + 2 * h->word_bytes + h->exponent_bytes; return TN_OK;
         default: return TN_ERR_INVALID_ARG;
     }
 }
