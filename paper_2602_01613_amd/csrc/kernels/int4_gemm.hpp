@@ -24,20 +24,28 @@ struct Int4GemmArgs {
     int32_t blocks_per_split;        // blocks of k to a range
 };
 
+// LDS: two or three stages of tokens; a ring of CODES blocks of 128 k of the waves' codes, and one of their scale words. (Transposed, a block's words are
+// read step by step, so that their ring has one block more.)
 template <int TM>
+constexpr int kInt4PerCU = TM <= 4 ? 2 : 1;
+template <int TM, bool TRANSPOSED, int SUB>
 struct Int4Shape {
-    static constexpr int BM = 16 * TM, STAGE = BM * 128, NS = 3, SMEM = NS * STAGE;
-    static constexpr int PER_CU = TM <= 4 ? 2 : 1;
+    static constexpr int BM = 16 * TM, STAGE = BM * 128, NS = TM == 4 ? 2 : 3;
+    static constexpr int CODES = TM >= 12 ? 4 : TM >= 8 ? 5 : 3;
+    static constexpr int WORDS = TRANSPOSED ? CODES + 1 : CODES;
+    static constexpr int WORD_LOADS = TRANSPOSED ? 2 * SUB : SUB, WAVE_WORDS = WORD_LOADS * 256;
+    static constexpr int CODES_AT = NS * STAGE, WORDS_AT = CODES_AT + CODES * 16384, SMEM = WORDS_AT + WORDS * 4 * WAVE_WORDS;
+    static_assert(kInt4PerCU<TM> * SMEM <= 160 * 1024, "LDS of a compute unit");
 };
 
 typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
 typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ floatx4 mfma16h(uintx4 w, halfx8 x, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(halfx8, w), x, c, 0, 0, 0); }
 
-// Two weights from element pair `pair` of a word of codes: 1024 + code is a code in the low bits of an fp16 1024, and all up to the product exact
-__device__ __forceinline__ unsigned weights_as_half(unsigned w, int pair, halfx2 scale, halfx2 offset) {
-    const halfx2 h = __builtin_bit_cast(halfx2, ((w >> (4 * pair)) & 0x000F000Fu) | 0x64006400u);
-    return __builtin_bit_cast(unsigned, (h + offset) * scale);
+// Two weights from element pair `pair` of a word, in three parts: 1024 + code, which is a code in the low bits of an fp16 1024; code - zero; the
+// product with the scale, which is the only one that rounds.
+__device__ __forceinline__ halfx2 codes_as_half(unsigned w, int pair, unsigned thousands) {
+    return __builtin_bit_cast(halfx2, ((w >> (4 * pair)) & 0x000F000Fu) | thousands);
 }
 
 template <int N>
@@ -50,22 +58,23 @@ __device__ __forceinline__ void for_constants(F&& f, std::integer_sequence<int, 
 }
 
 #ifdef __HIP_DEVICE_COMPILE__
-// keeps accumulators where they are across a loop's back edge: in the accumulation registers where they are more than half of all
+// Keeps accumulators in the accumulation registers: without it they change places from step to step, by moves where those are nearly full.
 template <int TM>
 __device__ __forceinline__ void pin(floatx4 (&acc)[TM][4]) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-            if constexpr (TM >= 8) asm volatile("" : "+a"(acc[i][f]));
+            if constexpr (kInt4PerCU<TM> == 1) asm volatile("" : "+a"(acc[i][f]));
             else asm volatile("" : "+v"(acc[i][f]));
         }
 }
 
 template <int TM, int FORM, bool TRANSPOSED, int SUB>
 __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
-    using S = Int4Shape<TM>;
+    using S = Int4Shape<TM, TRANSPOSED, SUB>;
     constexpr int LOADS = TM / 2;                 // of a stage, to a wave: 8 rows each
+    constexpr int W = 4 + S::WORD_LOADS;          // of a block's codes and words
     static_assert(TM % 2 == 0, "whole loads for each wave");
     typedef __attribute__((address_space(3))) void lds_t;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -92,11 +101,11 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
         const_cast<_Float16*>(static_cast<const _Float16*>(a.x) + int64_t(row_tile) * S::BM * a.x_stride), 0, (rows - 1) * row_bytes + a.k_blocks * (kBlock * 2), RSRC);
     const int vx = (wave * 8 + (lane >> 3)) * row_bytes + (((lane & 7) ^ ((wave & 1) * 4 + (lane >> 4))) * 16);
     const int last_stage = (kb0 + nk) * 2 - 1;
-    auto load_x = [&](int n, int at, unsigned char* s) {              // n: load of the stage; at: stage in memory
+    auto load_x = [&](int n, int at, unsigned char* s) {              // n: load of the stage; at: stage in memory (past the last: that one, not read)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_t*)(s + (wave + 4 * n) * 1024), 16, vx + n * 32 * row_bytes, min(at, last_stage) * 128, 0, 0);
     };
 
-    // the wave's four pieces: gated, two of gate's and the same two of up's
+    // the wave's four pieces: gated, two of gate's and the same two of up's; a wave that has none multiplies the first ones and stores nothing
     const int all_pieces = a.f_pieces * a.tensors;
     const int first = FORM == INT4_GATED ? col_tile * 8 + wave * 2 : col_tile * 16 + wave * 4;
     const bool there = FORM == INT4_GATED ? first < a.f_pieces : first < all_pieces;         // (pieces come in fours)
@@ -104,112 +113,146 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
         const int p = there ? first : 0;
         return FORM == INT4_GATED ? (f < 2 ? p + f : a.f_pieces + p + f - 2) : p + f;
     };
-    const unsigned* codes[4];
-    const unsigned* words[4];
+    const int piece_bytes = a.k_blocks * 1024;
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned*>(a.packed + int64_t(piece_of(0)) * a.k_blocks * kPieceWords), 0,
+                                                                        (FORM == INT4_GATED ? 2 : 4) * piece_bytes, RSRC);
+    const __amdgpu_buffer_rsrc_t ru = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned*>(a.packed + int64_t(piece_of(2)) * a.k_blocks * kPieceWords), 0,
+                                                                        2 * piece_bytes, RSRC);
+    // Words of a block. As it is: of the four pieces at a time, [group within the block][piece][feature]. Transposed: 128 k of a group of features, of which
+    // the wave has SUB (1 where groups are of 64 and more, 2 of 32).
+    const unsigned* const words0 = TRANSPOSED ? a.halves + piece_of(0) / a.group_pieces * a.word_stride : a.halves + int64_t(piece_of(0)) * a.k_blocks * (SUB * kPiece);
+    const int up_words = FORM == INT4_GATED ? (a.f_pieces - 2) * (a.k_blocks * SUB * kPiece * 4) : 0;       // from where a third piece would lie to where up's is
+    const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<unsigned*>(words0), 0, TRANSPOSED ? int(SUB * a.word_stride * 4) : 4 * a.k_blocks * (SUB * kPiece * 4) + up_words, RSRC);
+    const int vw = TRANSPOSED ? lane * 4 : (lane >> 4) * (a.k_blocks * SUB * kPiece * 4) + (lane & 15) * 4 + (lane >= 32 ? up_words : 0);
+    unsigned char* const codes_lds = smem + S::CODES_AT + wave * 4096;
+    unsigned char* const words_lds = smem + S::WORDS_AT + wave * S::WAVE_WORDS;
+    auto load_weights = [&](int kb, int code_slot, int word_slot) {       // kb: block of the range (past the last: that one, not read)
+        const int at = kb0 + min(kb, nk - 1);
+        unsigned char *c = codes_lds + code_slot, *w = words_lds + word_slot;
 #pragma unroll
-    for (int f = 0; f < 4; ++f) {
-        codes[f] = a.packed + int64_t(piece_of(f)) * a.k_blocks * kPieceWords + lane * 4;
-        words[f] = TRANSPOSED ? a.halves + piece_of(f) / a.group_pieces * a.word_stride + (lane >> 4) * 8
-                              : a.halves + int64_t(piece_of(f)) * a.k_blocks * (SUB * kPiece) + (lane & 15);
-    }
-    // Transposed: scales along k, the same for the pieces of a group, of which the wave has SUB (1 for groups of 64 and more, 2 for 32)
-    constexpr int NW = TRANSPOSED ? SUB : 4;
-    struct Words {
-        unsigned w[TRANSPOSED ? 1 : 4][TRANSPOSED ? 1 : SUB];
-    };
-    uintx4 now[4], next[4];
-    Words words_now, words_next;
-    auto load_codes = [&](uintx4 (&to)[4], Words& w, int kb) {
-        const int at = min(kb, kb0 + nk - 1);
+        for (int f = 0; f < 4; ++f)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(FORM == INT4_GATED && f >= 2 ? ru : rc, (lds_t*)(c + f * 1024), 16, lane * 16,
+                                                     (FORM == INT4_GATED ? f & 1 : f) * piece_bytes + at * 1024, 0, 0);
 #pragma unroll
-        for (int f = 0; f < 4; ++f) to[f] = *reinterpret_cast<const uintx4*>(codes[f] + int64_t(at) * kPieceWords);
-        if constexpr (!TRANSPOSED) {
-#pragma unroll
-            for (int f = 0; f < 4; ++f)
-#pragma unroll
-                for (int s = 0; s < SUB; ++s) w.w[f][s] = words[f][(int64_t(at) * SUB + s) * kPiece];
-        }
-    };
-    // transposed: scales and zeros of the lane's 8 k of a step
-    uintx4 kw[NW][2];
-    auto load_words = [&](int kb, int j) {
-        const int at = min(kb, kb0 + nk - 1);
-        if constexpr (TRANSPOSED) {
-#pragma unroll
-            for (int n = 0; n < NW; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) kw[n][h] = *reinterpret_cast<const uintx4*>(words[n * (4 / NW)] + int64_t(at) * kBlock + j * 32 + h * 4);
-        }
+        for (int n = 0; n < S::WORD_LOADS; ++n)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_t*)(w + n * 256), 4, vw,
+                                                     TRANSPOSED ? (n >> 1) * int(a.word_stride * 4) + at * 512 + (n & 1) * 256 : (at * SUB + n) * (kPiece * 4), 0, 0);
     };
 
     const int r = lane & 15, kq = lane >> 4;
     const int o0 = r * 128 + ((kq ^ (r >> 1)) * 16), o1 = r * 128 + (((4 + kq) ^ (r >> 1)) * 16);
     halfx8 fx[TM];
-    uintx4 fw[2][4];
+    uintx4 codes[4], fw[2][4];
+    unsigned words[TRANSPOSED ? 1 : 4][TRANSPOSED ? 1 : SUB];
+    uintx4 k_words[TRANSPOSED ? SUB : 1][2];
     floatx4 acc[TM][4];
     auto read_x = [&](int i, int half, const unsigned char* s) { fx[i] = *reinterpret_cast<const halfx8*>(s + (half ? o1 : o0) + i * 2048); };
-    // word `at` of the 16 (pair p of fragment f) of step j
-    auto make = [&](uintx4 (&to)[4], const uintx4 (&c)[4], const Words& w, int j, int at) {
-        const int f = at >> 2, p = at & 3;
-        if constexpr (TRANSPOSED) {
-            const int n = f / (4 / NW);
-            const unsigned scales = kw[n][0][p], offsets = kw[n][1][p];          // (a cast of the element itself takes the vector's first)
-            to[f][p] = weights_as_half(c[f][j], p, __builtin_bit_cast(halfx2, scales), __builtin_bit_cast(halfx2, offsets));
-        } else {
-            const halfx2 w2 = __builtin_bit_cast(halfx2, w.w[f][j * SUB / 4]);
-            to[f][p] = weights_as_half(c[f][j], p, halfx2{w2[0], w2[0]}, halfx2{w2[1], w2[1]});
+    auto read_codes = [&](int code_slot, int word_slot) {
+#pragma unroll
+        for (int f = 0; f < 4; ++f) codes[f] = *reinterpret_cast<const uintx4*>(codes_lds + code_slot + f * 1024 + lane * 16);
+        if constexpr (!TRANSPOSED) {
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+#pragma unroll
+                for (int s = 0; s < SUB; ++s) words[f][s] = *reinterpret_cast<const unsigned*>(words_lds + word_slot + s * 256 + f * 64 + r * 4);
         }
     };
-
-    load_codes(now, words_now, kb0);
-    load_words(kb0, 0);
+    auto read_k_words = [&](int word_slot, int j) {                       // transposed: scales and offsets of the lane's 8 k of a step
+        if constexpr (TRANSPOSED) {
 #pragma unroll
-    for (int q = 0; q < S::NS; ++q)
+            for (int n = 0; n < SUB; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) k_words[n][h] = *reinterpret_cast<const uintx4*>(words_lds + word_slot + n * 512 + j * 128 + kq * 32 + h * 16);
+        }
+    };
+    unsigned thousands = 0x64006400u;             // 1024 twice, in a register: with the mask in another the two are one instruction
+    asm volatile("" : "+v"(thousands));
+    // part 0, 1 or 2 of word `at` of the 16 (pair p of fragment f) of step j
+    halfx2 half_made[16];
+    auto make = [&](uintx4 (&to)[4], int j, int at, int part) {
+        const int f = at >> 2, p = at & 3;
+        halfx2 scale, offset;
+        if constexpr (TRANSPOSED) {
+            const unsigned scales = k_words[f * SUB / 4][0][p], offsets = k_words[f * SUB / 4][1][p];          // (a cast of the element itself takes the vector's first)
+            scale = __builtin_bit_cast(halfx2, scales);
+            offset = __builtin_bit_cast(halfx2, offsets);
+        } else {
+            const halfx2 w2 = __builtin_bit_cast(halfx2, words[f][j * SUB / 4]);
+            scale = halfx2{w2[0], w2[0]};
+            offset = halfx2{w2[1], w2[1]};
+        }
+        if (part == 0) half_made[at] = codes_as_half(codes[f][j], p, thousands);
+        else if (part == 1) half_made[at] = half_made[at] + offset;
+        else to[f][p] = __builtin_bit_cast(unsigned, half_made[at] * scale);
+    };
+
+    // Loads are counted: every block brings LOADS of tokens, W of codes and words, and LOADS of tokens again, in this order. What is waited for in the middle of a stage
+    // is the next one, and all that was requested before it.
+    constexpr int NEWER_FIRST = S::NS == 3 ? W + LOADS : 0, NEWER_SECOND = S::NS == 3 ? W + LOADS : W;
+    constexpr int WORD_STEP = 4 * S::WAVE_WORDS;
+    load_weights(0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
         for (int n = 0; n < LOADS; ++n) load_x(n, kb0 * 2 + q, smem + q * S::STAGE);
+    load_weights(1, 16384, WORD_STEP);
+    if constexpr (S::NS == 3) {
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) load_x(n, kb0 * 2 + 2, smem + 2 * S::STAGE);
+    }
+#pragma unroll
+    for (int q = 2; q < S::CODES; ++q) load_weights(q, q * 16384, q * WORD_STEP);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int f = 0; f < 4; ++f) acc[i][f] = floatx4{0.f, 0.f, 0.f, 0.f};
     pin(acc);
-#pragma unroll
-    for (int at = 0; at < 16; ++at) make(fw[0], now, words_now, 0, at);
-    load_words(kb0, 1);
-    wait_vmcnt<(S::NS - 1) * LOADS>();
+    __builtin_amdgcn_sched_barrier(0);
+    wait_vmcnt<(S::NS - 1) * LOADS + (S::CODES - 1) * W>();
     __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    read_codes(0, 0);
+    read_k_words(0, 0);
+#pragma unroll
+    for (int at = 0; at < 48; ++at) make(fw[0], 0, at / 3, at % 3);
+    read_k_words(0, 1);
 #pragma unroll
     for (int i = 0; i < TM; ++i) read_x(i, 0, smem);
 
-    int stage = 0;                                // of the current 64 k, in bytes
+    int stage = 0, code_slot = 0, word_slot = 0;  // of the current 64 k and block, in bytes
     for (int kb = 0; kb < nk; ++kb) {
-        load_codes(next, words_next, kb0 + kb + 1);
+        const int next_code_slot = code_slot == (S::CODES - 1) * 16384 ? 0 : code_slot + 16384;
+        const int next_word_slot = word_slot == (S::WORDS - 1) * WORD_STEP ? 0 : word_slot + WORD_STEP;
         auto step = [&](auto j_c) {
             constexpr int j = decltype(j_c)::value, half = j & 1;
             unsigned char* s = smem + stage;
             const int after = stage == (S::NS - 1) * S::STAGE ? 0 : stage + S::STAGE;
             unsigned char* sn = smem + after;
-            constexpr int BAR = TM > 2 ? 2 : 1;   // second half: reads start behind the barrier, which is in front of this fragment
+            // second half: the barrier is in front of this fragment, and reads of the next stage (in the last step, of the next codes too) behind it
+            constexpr int BAR = TM > 4 ? 2 : TM > 2 ? 1 : 0;
+            // The 16 words of the next step, dealt over these fragments: a word's three parts need each other, so that each goes to a slot of its own,
+            // beside others' (one after another in one slot, the next MFMA waits for all of them).
+            constexpr int FROM = j == 3 ? BAR + 1 : 0, SLOTS = 4 * (TM - FROM);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
                 if (half && i == BAR) {
-                    __builtin_amdgcn_s_waitcnt(0xC07F);                // lgkmcnt(0): this wave has read what it reads of the stage
-                    // The next stage has landed: behind it only the one after it was requested for certain (the compiler is free to
-                    // move the loads of codes, which can only make this wait longer).
-                    wait_vmcnt<LOADS>();
+                    __builtin_amdgcn_s_waitcnt(0xC07F);                // lgkmcnt(0): this wave has read what it reads of the stage, and its codes
+                    wait_vmcnt<j == 1 ? NEWER_FIRST : NEWER_SECOND>();  // the next stage, and the next block's codes, have landed
                     __builtin_amdgcn_s_barrier();
                     __builtin_amdgcn_sched_barrier(0);
+                    if (j == 3) read_codes(next_code_slot, next_word_slot);
                 }
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
                     acc[i][f] = mfma16h(fw[half][f], fx[i], acc[i][f]);
-                    const int slot = i * 4 + f;
+                    const int slot = (i - FROM) * 4 + f;
 #pragma unroll
-                    for (int at = 0; at < 16; ++at)              // the 16 words, dealt over the slots
-                        if ((TM < 4 ? at * TM / 4 : (at + 1) * TM / 4 - 1) == slot) {
-                            if (j == 3) make(fw[0], next, words_next, 0, at);
-                            else make(fw[1 - half], now, words_now, j + 1, at);
-                        }
+                    for (int at = 0; at < 16; ++at)
+#pragma unroll
+                        for (int part = 0; part < 3; ++part)
+                            if (i >= FROM && at * (SLOTS - 2) / 16 + part == slot) make(fw[1 - half], (j + 1) & 3, at, part);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (!half) {
@@ -220,14 +263,15 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
                         for (int q = 0; q < BAR; ++q) read_x(q, 0, sn);
                     }
                     read_x(i, 0, sn);
-                    // the stage's loads, dealt over the rest of the step
+                    // the stage's loads, dealt over the rest of the step; in the first second half the codes' behind them
 #pragma unroll
                     for (int n = 0; n < LOADS; ++n)
                         if (BAR + n * (TM - BAR) / LOADS == i) load_x(n, (kb0 + kb) * 2 + (j >> 1) + S::NS, s);
+                    if (j == 1 && i == TM - 1) load_weights(kb + S::CODES, code_slot, TRANSPOSED ? (word_slot == 0 ? (S::WORDS - 1) * WORD_STEP : word_slot - WORD_STEP) : word_slot);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (TRANSPOSED) load_words(kb0 + kb + (j >= 2 ? 1 : 0), (j + 2) & 3);
+            read_k_words(j >= 2 ? next_word_slot : word_slot, (j + 2) & 3);
             if (half) stage = after;
             pin(acc);
         };
@@ -235,9 +279,8 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
         step(std::integral_constant<int, 1>());
         step(std::integral_constant<int, 2>());
         step(std::integral_constant<int, 3>());
-#pragma unroll
-        for (int f = 0; f < 4; ++f) now[f] = next[f];
-        words_now = words_next;
+        code_slot = next_code_slot;
+        word_slot = next_word_slot;
     }
     wait_vmcnt<0>();                              // no load into LDS outlives the workgroup
     if (!there) return;
@@ -279,7 +322,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
 #endif
 
 template <int TM, int FORM, bool TRANSPOSED, int SUB>
-__global__ void __launch_bounds__(256, Int4Shape<TM>::PER_CU) int4_gemm_kernel(Int4GemmArgs g) {
+__global__ void __launch_bounds__(256, kInt4PerCU<TM>) int4_gemm_kernel(Int4GemmArgs g) {
 #ifdef __HIP_DEVICE_COMPILE__
     int4_tile<TM, FORM, TRANSPOSED, SUB>(g);
 #endif

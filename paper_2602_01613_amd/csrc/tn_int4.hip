@@ -125,7 +125,7 @@ Int4Args product_args(const tn_int4_linear_s& h, const void* x, int64_t x_stride
 // which kernel a product runs on
 // ---------------------------------------------------------------------------------------------
 constexpr int64_t kStreamTokens = 64;           // streamed up to here
-constexpr int kTileTokens[] = {2, 4, 8, 12};       // TM
+constexpr int kTileTokens[] = {2, 4, 8, 12};    // TM
 
 struct Choice {
     int tm = 0;                // tile of 16 * tm tokens; 0: streamed
@@ -188,7 +188,7 @@ int stream_form(const Int4Args& a, bool gated, hipStream_t stream) {
 template <int TM, int FORM, bool TRANSPOSED, int SUB>
 int run_gemm(const Int4GemmArgs& g, hipStream_t stream) {
     const int64_t items = int64_t(g.n_row) * g.n_col * g.l.n_split;
-    int4_gemm_kernel<TM, FORM, TRANSPOSED, SUB><<<dim3(unsigned(div_up(items, 8) * 8)), dim3(256), Int4Shape<TM>::SMEM, stream>>>(g);
+    int4_gemm_kernel<TM, FORM, TRANSPOSED, SUB><<<dim3(unsigned(div_up(items, 8) * 8)), dim3(256), Int4Shape<TM, TRANSPOSED, SUB>::SMEM, stream>>>(g);
     return launched();
 }
 template <int TM, int FORM>
@@ -223,7 +223,7 @@ int run_tiles(const Int4Args& a, bool gated, hipStream_t stream) {
 template <int TM, int FORM, bool TRANSPOSED, int SUB>
 bool allow() {          // more LDS than a launch gets by default
     return hipFuncSetAttribute(reinterpret_cast<const void*>(int4_gemm_kernel<TM, FORM, TRANSPOSED, SUB>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               Int4Shape<TM>::SMEM) == hipSuccess;
+                               Int4Shape<TM, TRANSPOSED, SUB>::SMEM) == hipSuccess;
 }
 template <int TM>
 bool allow_tiles() {
