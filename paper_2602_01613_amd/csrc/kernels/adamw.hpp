@@ -67,20 +67,31 @@ __device__ __forceinline__ double group_sum64(double v, double* part) {
 __global__ void __launch_bounds__(256) gradient_norm_kernel(AdamwArgs a, Gradients g, double* sums) {
     __shared__ double part[4];
     double sum = 0;
+    // (the next part's tables are read while this one's values are under way: without that, three loads wait for each other)
+    PartEntry e{};
+    TensorEntry t{};
+    if (blockIdx.x < a.n_parts) {
+        e = a.parts[blockIdx.x];
+        t = a.tensors[e.tensor];
+    }
     for (int64_t c = blockIdx.x; c < a.n_parts; c += gridDim.x) {
-        const PartEntry e = a.parts[c];
-        const TensorEntry t = a.tensors[e.tensor];
         const void* p = g.at(e.tensor);
         const bool bf16 = g.is_bf16(e.tensor);
+        const int64_t at0 = int64_t(e.part) * kPartValues + int(threadIdx.x) * kChunk;
+        float v[kPartValues / (256 * kChunk)][kChunk];
 #pragma unroll
         for (int i = 0; i < kPartValues / (256 * kChunk); ++i) {
-            const int64_t at = int64_t(e.part) * kPartValues + (i * 256 + int(threadIdx.x)) * kChunk, left = t.size - at;
-            if (left <= 0) continue;
-            float v[kChunk];
-            load_values(p, bf16, at, int(left < kChunk ? left : kChunk), v);
-#pragma unroll
-            for (int q = 0; q < kChunk; ++q) sum += double(v[q]) * double(v[q]);
+            const int64_t at = at0 + i * 256 * kChunk, left = t.size - at;
+            load_values(p, bf16, left > 0 ? at : 0, int(left < 0 ? 0 : left < kChunk ? left : kChunk), v[i]);
         }
+        if (c + gridDim.x < a.n_parts) {
+            e = a.parts[c + gridDim.x];
+            t = a.tensors[e.tensor];
+        }
+#pragma unroll
+        for (int i = 0; i < kPartValues / (256 * kChunk); ++i)
+#pragma unroll
+            for (int q = 0; q < kChunk; ++q) sum += double(v[i][q]) * double(v[i][q]);
     }
     sum = group_sum64(sum, part);
     if (threadIdx.x == 0) sums[blockIdx.x] = sum;

@@ -31,7 +31,7 @@ constexpr int kInt4PerCU = TM <= 4 ? 2 : 1;
 template <int TM, bool TRANSPOSED, int SUB>
 struct Int4Shape {
     static constexpr int BM = 16 * TM, STAGE = BM * 128, NS = TM == 4 ? 2 : 3;
-    static constexpr int CODES = TM >= 12 ? 4 : TM >= 8 ? 5 : 3;
+    static constexpr int CODES = TM >= 10 ? 4 : TM >= 6 ? 5 : 3;
     static constexpr int WORDS = TRANSPOSED ? CODES + 1 : CODES;
     static constexpr int WORD_LOADS = TRANSPOSED ? 2 * SUB : SUB, WAVE_WORDS = WORD_LOADS * 256;
     static constexpr int CODES_AT = NS * STAGE, WORDS_AT = CODES_AT + CODES * 16384, SMEM = WORDS_AT + WORDS * 4 * WAVE_WORDS;

@@ -16,7 +16,7 @@ namespace {
 static_assert(TN_ADAMW_BLOCK == kBlock, "states share the 8-bit format of rows");
 
 constexpr int64_t kMostValues = int64_t(1) << 40;
-constexpr int kNormGroups = 1024;                // workgroups of the norm, over all its launches
+constexpr int kNormGroups = 2048;                // workgroups of the norm, over all its launches
 constexpr int64_t kLaunchParts = int64_t(1) << 22;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -124,65 +124,89 @@ Int4Args product_args(const tn_int4_linear_s& h, const void* x, int64_t x_stride
 // ---------------------------------------------------------------------------------------------
 // which kernel a product runs on
 // ---------------------------------------------------------------------------------------------
-constexpr int64_t kStreamTokens = 64;           // streamed up to here
-constexpr int kTileTokens[] = {2, 4, 8, 12};    // TM
+// Times in us, fitted to measurements on the MI355X (256 CUs) of products of 5120 to 51200 inputs and 1024 to 51200 outputs, 1 to 8192 tokens.
+constexpr int64_t kStreamTokens = 64;           // streamed up to here at the most
+struct TileCost {
+    int tm, per_cu;
+    double alone, full;        // a block of 128 k: of one workgroup on a CU, and of as many as there is room for
+};
+constexpr TileCost kTiles[] = {{2, 2, 0.88, 1.5}, {4, 2, 1.15, 1.95}, {6, 1, 1.45, 1.5}, {8, 1, 1.75, 1.83}, {10, 1, 2.05, 2.12}, {12, 1, 2.4, 2.5}};
+constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24};
+constexpr int64_t kMostSums = int64_t(128) << 20;
+constexpr double kLaunch = 4.0, kTileRest = 3.0, kReadRate = 4.5e6, kCachedRate = 25e6, kSumsRate = 8e6, kRowsRate = 4e6;      // bytes per us
+constexpr double kStreamRows = 36e3;            // bytes of tokens that a CU's streaming workgroups read in a us
+// Memory and computation overlap, but not wholly: of the shorter one this much is added.
+double together(double a, double b) { return a > b ? a + 0.35 * b : b + 0.35 * a; }
 
 struct Choice {
     int tm = 0;                // tile of 16 * tm tokens; 0: streamed
     int split = 1;
     int groups = 2, tg = 1;    // streamed: pieces and 16s of tokens to a workgroup
+    int waves = 4;
+    double us = 1e30;
 };
 
-Choice choose(const Int4Args& a, bool gated) {
+// Pieces of a streaming workgroup: one where a token's worth of rows is read and each CU gets few (1024 outputs of 5120 inputs, one token: 6.3 us, 7.7 with two);
+// four where more tokens are read, once for all of its pieces, and each CU has a workgroup or more (25600 outputs, 16 tokens: 21 us, 30 with two).
+// Waves: four, so that a CU has several workgroups, one of them at its beginning or end while others stream (gated 25600 outputs, one token: 35 us, 45 with eight);
+// eight where there are fewer workgroups than CUs and little else to read (25600 -> 5120, one token: 19 us, 22 with four).
+Choice choose_stream(const Int4Args& a, bool gated, int64_t pieces) {
     Choice c;
-    const int64_t pieces = int64_t(a.f_pieces) * a.tensors;
-    if (a.tokens <= kStreamTokens && !a.transpose) {
-        c.tg = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-        return c;
-    }
-    const int64_t n_col = div_up(gated ? pieces / 2 : pieces, gated ? 8 : 16);
-    double best = 1e30;
-    for (const int tm : kTileTokens) {
-        const int64_t n_row = div_up(a.tokens, 16 * tm);
-        for (const int split : {1, 2, 3, 4, 6, 8}) {
-            if (split > 1 && split * 4 > a.k_blocks) break;
-            const int64_t blocks = div_up(a.k_blocks, split), items = n_row * n_col * div_up(a.k_blocks, blocks);
-            const int per_cu = tm <= 4 ? 2 : 1;
-            const double k_block = tm == 2 ? 0.4 : tm == 4 ? 0.62 : tm == 8 ? 1.0 : 1.4;          // us of a workgroup, with per_cu on a CU
-            double us = div_up(items, kCUs * per_cu) * (blocks * k_block + 3.0);
-            if (split > 1) us += 4.0 + double(a.tokens) * a.ld * 4 * 2 * split / 5e6;
-            if (us < best) {
-                best = us;
-                c.tm = tm;
-                c.split = split;
-            }
-        }
-    }
+    c.tg = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
+    c.groups = c.tg > 1 ? 2 : a.tokens <= 4 ? (!gated && pieces <= 2 * kCUs && a.k_blocks < 100 ? 1 : 2) : pieces >= 4 * kCUs ? 4 : 2;
+    const int64_t groups = pieces / c.groups;
+    c.waves = groups < kCUs && a.tokens <= 4 ? 8 : 4;
+    const double weight = double(pieces) * a.k_blocks * (1024 + 64 * a.sub), per_cu = groups < kCUs ? 1.0 : double(groups) / kCUs;
+    const int64_t read = c.tg > 1 ? 16 * c.tg : a.tokens;         // (16 at a time, of which those past the last are all the last one)
+    c.us = kLaunch + together(weight / kReadRate, per_cu * read * a.k_blocks * (kBlock * 2) / kStreamRows);
     return c;
 }
 
-// Waves of a workgroup of the stream kernel: the number up to 8 that leaves the fewest of them idle in the last round
-int stream_waves(int rounds) {
-    int best = rounds < 8 ? rounds : 8;
-    for (int w = best - 1; w >= 4; --w)
-        if (div_up(rounds, w) * w < div_up(rounds, best) * best) best = w;
+Choice choose(const Int4Args& a, bool gated) {
+    const int64_t pieces = int64_t(a.f_pieces) * a.tensors;
+    Choice best;
+    if (a.tokens <= kStreamTokens && !a.transpose) best = choose_stream(a, gated, pieces);
+    const double weight = double(pieces) * a.k_blocks * (1024 + 64 * a.sub), rows = double(a.tokens) * a.k_blocks * (kBlock * 4), outputs = double(a.tokens) * a.ld * 4;
+    const int64_t n_col = div_up(gated ? pieces / 2 : pieces, gated ? 8 : 16);
+    for (const TileCost& t : kTiles) {
+        const int64_t n_row = div_up(a.tokens, 16 * t.tm);
+        for (const int split : kSplits) {
+            if (split > 1 && (split * 4 > a.k_blocks || split * outputs > double(kMostSums))) break;
+            const int64_t blocks = div_up(a.k_blocks, split), cols = gated && split > 1 ? div_up(pieces, 16) : n_col, items = n_row * cols * div_up(a.k_blocks, blocks);
+            const int64_t held = items <= kCUs ? kCUs : int64_t(kCUs) * t.per_cu;
+            const double compute = double(div_up(items, held)) * (double(blocks) * (items <= kCUs ? t.alone : t.full) + kTileRest);
+            const double memory = weight / kReadRate + double(n_row - 1) * weight / kCachedRate;
+            const double us = kLaunch + 3.0 + rows / kRowsRate + together(compute, memory) + (split > 1 ? 3.0 + 2 * split * outputs / kSumsRate : 0);
+            if (us < best.us) {
+                best = Choice();
+                best.us = us;
+                best.tm = t.tm;
+                best.split = split;
+            }
+        }
+    }
     return best;
 }
 
 template <int GROUPS, int TG, int SUB, bool GATED>
-int run_stream(const Int4Args& a, hipStream_t stream) {
+int run_stream(const Int4Args& a, int waves, hipStream_t stream) {
     constexpr int OWN = GATED ? GROUPS / 2 : GROUPS;
     const dim3 grid(unsigned((GATED ? a.f_pieces : int64_t(a.f_pieces) * a.tensors) / OWN), unsigned(div_up(a.tokens, 16 * TG)));
-    int4_stream_kernel<GROUPS, TG, SUB, GATED><<<grid, dim3(64 * stream_waves(a.k_blocks)), 0, stream>>>(a);
+    int4_stream_kernel<GROUPS, TG, SUB, GATED><<<grid, dim3(unsigned(64 * (waves < a.k_blocks ? waves : a.k_blocks))), 0, stream>>>(a);
     return launched();
 }
-template <int GROUPS, int TG>
-int stream_form(const Int4Args& a, bool gated, hipStream_t stream) {
-    switch (a.sub) {
-        case 1: return gated ? run_stream<GROUPS, TG, 1, true>(a, stream) : run_stream<GROUPS, TG, 1, false>(a, stream);
-        case 2: return gated ? run_stream<GROUPS, TG, 2, true>(a, stream) : run_stream<GROUPS, TG, 2, false>(a, stream);
-        default: return gated ? run_stream<GROUPS, TG, 4, true>(a, stream) : run_stream<GROUPS, TG, 4, false>(a, stream);
+template <int GROUPS, int TG, int SUB>
+int stream_form(const Int4Args& a, const Choice& c, bool gated, hipStream_t stream) {
+    if constexpr (GROUPS > 1) {
+        if (gated) return run_stream<GROUPS, TG, SUB, true>(a, c.waves, stream);
     }
+    return run_stream<GROUPS, TG, SUB, false>(a, c.waves, stream);
+}
+template <int SUB>
+int stream_sizes(const Int4Args& a, const Choice& c, bool gated, hipStream_t stream) {
+    if (c.tg == 4) return stream_form<2, 4, SUB>(a, c, gated, stream);
+    if (c.tg == 2) return stream_form<2, 2, SUB>(a, c, gated, stream);
+    return c.groups == 1 ? stream_form<1, 1, SUB>(a, c, gated, stream) : c.groups == 2 ? stream_form<2, 1, SUB>(a, c, gated, stream) : stream_form<4, 1, SUB>(a, c, gated, stream);
 }
 
 template <int TM, int FORM, bool TRANSPOSED, int SUB>
@@ -296,13 +320,15 @@ int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void
         a.x = workspace;
         a.x_stride = h.k_blocks * kBlock;
     }
-    if (c.tm == 0) return c.tg == 1 ? stream_form<2, 1>(a, gated, stream) : c.tg == 2 ? stream_form<2, 2>(a, gated, stream) : stream_form<2, 4>(a, gated, stream);
+    if (c.tm == 0) return a.sub == 1 ? stream_sizes<1>(a, c, gated, stream) : a.sub == 2 ? stream_sizes<2>(a, c, gated, stream) : stream_sizes<4>(a, c, gated, stream);
     a.n_split = c.split;
     if (c.split > 1) a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.rows + w.exponents);
     switch (c.tm) {
         case 2: return run_tiles<2>(a, gated, stream);
         case 4: return run_tiles<4>(a, gated, stream);
+        case 6: return run_tiles<6>(a, gated, stream);
         case 8: return run_tiles<8>(a, gated, stream);
+        case 10: return run_tiles<10>(a, gated, stream);
         default: return run_tiles<12>(a, gated, stream);
     }
 }
@@ -326,7 +352,7 @@ int tn_int4_linear_create(tn_int4_linear_t* out, const tn_int4_linear_desc* d) {
     lay_out(*d, *h);
     const hipStream_t st = static_cast<hipStream_t>(d->stream);
     const int64_t row_bytes = div_up(h->n, 2);
-    int rc = allow_tiles<2>() && allow_tiles<4>() && allow_tiles<8>() && allow_tiles<12>() ? TN_OK : TN_ERR_HIP;
+    int rc = allow_tiles<2>() && allow_tiles<4>() && allow_tiles<6>() && allow_tiles<8>() && allow_tiles<10>() && allow_tiles<12>() ? TN_OK : TN_ERR_HIP;
     // (what is quantised here passes through the form that a caller gives)
     unsigned char* made = nullptr;
     const int64_t scales_at = whole(h->m * row_bytes), zeros_at = scales_at + whole(h->m * h->groups * 2);
