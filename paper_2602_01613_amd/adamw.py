@@ -14,7 +14,7 @@ from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 
-from .binding import load_library
+from .binding import TN_DTYPE_BF16, TN_DTYPE_F32, load_library
 from .fp8 import _CODES, _DTYPE, _SCALES, _check, _here, _stream
 
 TN_ADAMW_BLOCK = 128
@@ -105,7 +105,8 @@ class AdamW:
         device = params[0].device
         self.params, self.lr, self.betas, self.eps, self.weight_decay = params, float(lr), (float(betas[0]), float(betas[1])), float(eps), decays
         self.state_bits, self.seed, self._gpu, self._device = int(state_bits), int(seed), gpu, device
-        self._sizes = [p.numel() for p in params]
+        self._sizes, self._shapes = [p.numel() for p in params], [p.shape for p in params]
+        self._all_f32 = (ctypes.c_int32 * len(params))(*[TN_DTYPE_F32] * len(params))
         values = _state_values(self._sizes)
         kind = torch.float32 if state_bits == 32 else _CODES
         new = lambda n, dtype: torch.zeros((n,), dtype=torch.uint8 if dtype.itemsize == 1 else dtype, device=device).view(dtype)      # noqa: E731
@@ -149,18 +150,27 @@ class AdamW:
 
     def _gradients(self, grads: Sequence[torch.Tensor]):
         self._open()
+        n, gpu, f32, bf16 = len(self._shapes), self._gpu, torch.float32, torch.bfloat16
         grads = list(grads)
-        n, gpu = len(self.params), self._gpu
         if len(grads) != n:
             raise ValueError(f"{len(grads)} gradients for {n} parameters")
-        pointers, codes = [], []
-        for i, (g, p) in enumerate(zip(grads, self.params)):
-            code = _DTYPE.get(g.dtype) if isinstance(g, torch.Tensor) else None
-            if code is None or g.shape != p.shape or g.get_device() != gpu or not g.is_contiguous():
-                raise ValueError(f"gradient {i} must be a contiguous {tuple(p.shape)} tensor of float32 or bfloat16 on GPU {gpu}")
+        pointers, halves = [], []
+        # (for hundreds of tensors this loop is most of a call's time on the host: as little as it takes)
+        for g, shape in zip(grads, self._shapes):
+            if not isinstance(g, torch.Tensor) or g.shape != shape or g.get_device() != gpu or not g.is_contiguous():
+                raise ValueError(f"gradient {len(pointers)} must be a contiguous {tuple(shape)} tensor of float32 or bfloat16 on GPU {gpu}")
+            dtype = g.dtype
+            if dtype is not f32:
+                if dtype is not bf16:
+                    raise ValueError(f"gradient {len(pointers)} must be of float32 or bfloat16, not {dtype}")
+                halves.append(len(pointers))
             pointers.append(g.data_ptr())
-            codes.append(code)
-        return (ctypes.c_void_p * n)(*pointers), (ctypes.c_int32 * n)(*codes)
+        codes = self._all_f32
+        if halves:
+            codes = (ctypes.c_int32 * n)()              # (TN_DTYPE_F32 is 0)
+            for i in halves:
+                codes[i] = TN_DTYPE_BF16
+        return (ctypes.c_void_p * n)(*pointers), codes
 
     def _space(self) -> torch.Tensor:
         return torch.empty((self._workspace_bytes,), dtype=torch.uint8, device=self._device)

@@ -80,7 +80,7 @@ struct StreamBlock {
     bf16x8 x[TG][4];
 };
 template <int TG>
-constexpr int kRing = TG == 4 ? 2 : TG == 2 ? 3 : 4;
+constexpr int kRing = TG == 2 ? 3 : 4;
 
 template <int GROUPS, int TG, int SUB, bool GATED>
 __global__ void __launch_bounds__(512) int4_stream_kernel(Int4Args a) {

@@ -134,7 +134,7 @@ constexpr TileCost kTiles[] = {{2, 2, 0.88, 1.5}, {4, 2, 1.15, 1.95}, {6, 1, 1.4
 constexpr int kSplits[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24};
 constexpr int64_t kMostSums = int64_t(128) << 20;
 constexpr double kLaunch = 4.0, kTileRest = 3.0, kReadRate = 4.5e6, kCachedRate = 25e6, kSumsRate = 8e6, kRowsRate = 4e6;      // bytes per us
-constexpr double kStreamRows = 36e3;            // bytes of tokens that a CU's streaming workgroups read in a us
+constexpr double kRowReadRate = 6e6, kRowPairReadRate = 7.5e6, kRowsAgainRate = 7e6, kOneCuRate = 32e3;      // of tokens by streaming workgroups; of the weight for their further tokens; of the weight by one CU
 // Memory and computation overlap, but not wholly: of the shorter one this much is added.
 double together(double a, double b) { return a > b ? a + 0.35 * b : b + 0.35 * a; }
 
@@ -146,20 +146,37 @@ struct Choice {
     double us = 1e30;
 };
 
-// Pieces of a streaming workgroup: one where a token's worth of rows is read and each CU gets few (1024 outputs of 5120 inputs, one token: 6.3 us, 7.7 with two);
-// four where more tokens are read, once for all of its pieces, and each CU has a workgroup or more (25600 outputs, 16 tokens: 21 us, 30 with two).
-// Waves: four, so that a CU has several workgroups, one of them at its beginning or end while others stream (gated 25600 outputs, one token: 35 us, 45 with eight);
-// eight where there are fewer workgroups than CUs and little else to read (25600 -> 5120, one token: 19 us, 22 with four).
+// A streaming workgroup's pieces (GROUPS), tokens (16 * TG) and waves. Every workgroup reads its tokens anew, 64 bytes of 16 rows to a load, which come at 5 to 6 TB/s in
+// all: with more tokens more pieces (25600 outputs of 5120 inputs, 16 tokens: 21 us with four, 31 with two, 46 with one), and 32 tokens at a time. Where there are few
+// outputs, a workgroup's own time counts, the blocks of k that its waves take one after another: one piece (1024 outputs, 64 tokens: 11 us, 20 with 64 tokens to a workgroup), and
+// eight waves instead of four (25600 -> 5120, one token: 19 us, 22 with four). Elsewhere four, so that a CU has several workgroups, one of them at its beginning or
+// end while others stream (gated 25600 outputs, one token: 35 us, 45 with eight).
+constexpr struct {
+    int groups, tg;
+} kStreams[] = {{1, 1}, {2, 1}, {4, 1}, {4, 2}};
+
 Choice choose_stream(const Int4Args& a, bool gated, int64_t pieces) {
-    Choice c;
-    c.tg = a.tokens <= 16 ? 1 : a.tokens <= 32 ? 2 : 4;
-    c.groups = c.tg > 1 ? 2 : a.tokens <= 4 ? (!gated && pieces <= 2 * kCUs && a.k_blocks < 100 ? 1 : 2) : pieces >= 4 * kCUs ? 4 : 2;
-    const int64_t groups = pieces / c.groups;
-    c.waves = groups < kCUs && a.tokens <= 4 ? 8 : 4;
-    const double weight = double(pieces) * a.k_blocks * (1024 + 64 * a.sub), per_cu = groups < kCUs ? 1.0 : double(groups) / kCUs;
-    const int64_t read = c.tg > 1 ? 16 * c.tg : a.tokens;         // (16 at a time, of which those past the last are all the last one)
-    c.us = kLaunch + together(weight / kReadRate, per_cu * read * a.k_blocks * (kBlock * 2) / kStreamRows);
-    return c;
+    Choice best;
+    const double weight = double(pieces) * a.k_blocks * (1024 + 64 * a.sub);
+    for (const auto& form : kStreams) {
+        if (gated && form.groups == 1) continue;
+        const int64_t tiles = div_up(a.tokens, 16 * form.tg), groups = pieces / form.groups * tiles;
+        const double rows = double(groups) * (tiles > 1 || form.tg > 1 ? 16 * form.tg : a.tokens) * a.k_blocks * (kBlock * 2);
+        const double one_cu = weight * double(tiles) / (double(groups < kCUs ? groups : kCUs) * kOneCuRate);
+        const double read = weight / kReadRate + double(tiles - 1) * weight / kRowsAgainRate, memory = read > one_cu ? read : one_cu;
+        for (const int waves : {4, 8}) {
+            if (waves == 8 && (groups > kCUs || a.k_blocks < 100)) break;
+            const double chain = (3.0 + double(div_up(a.k_blocks, waves)) * (0.13 + 0.1 * form.groups)) * (groups > 3 * kCUs ? double(groups) / (3 * kCUs) : 1.0);
+            const double shared = together(memory, rows / (form.tg > 1 ? kRowPairReadRate : kRowReadRate)), us = kLaunch + 1.0 + (chain > shared ? chain : shared);
+            if (us < 0.97 * best.us) {          // (of forms as good as each other the one with more workgroups)
+                best.us = us;
+                best.groups = form.groups;
+                best.tg = form.tg;
+                best.waves = waves;
+            }
+        }
+    }
+    return best;
 }
 
 Choice choose(const Int4Args& a, bool gated) {
@@ -204,8 +221,7 @@ int stream_form(const Int4Args& a, const Choice& c, bool gated, hipStream_t stre
 }
 template <int SUB>
 int stream_sizes(const Int4Args& a, const Choice& c, bool gated, hipStream_t stream) {
-    if (c.tg == 4) return stream_form<2, 4, SUB>(a, c, gated, stream);
-    if (c.tg == 2) return stream_form<2, 2, SUB>(a, c, gated, stream);
+    if (c.tg == 2) return stream_form<4, 2, SUB>(a, c, gated, stream);
     return c.groups == 1 ? stream_form<1, 1, SUB>(a, c, gated, stream) : c.groups == 2 ? stream_form<2, 1, SUB>(a, c, gated, stream) : stream_form<4, 1, SUB>(a, c, gated, stream);
 }
 
