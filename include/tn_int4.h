@@ -15,7 +15,7 @@
  *     number (ties to even), limited to 0 .. 15;  a group of scale 0 has zero = code = 8
  * A group that holds an infinity or a NaN gets the scale NaN, zero = code = 8, so that the fault shows wherever the group is used.
  *
- * Tokens: up to 2^30 a call; features up to TN_INT4_MAX_FEATURES per tensor and side. More is TN_ERR_UNSUPPORTED.
+ * Tokens: up to 2^30 a call; features up to TN_INT4_MAX_FEATURES per tensor and side, TN_INT4_MAX_WEIGHTS together. More is TN_ERR_UNSUPPORTED.
  */
 #ifndef TN_INT4_H
 #define TN_INT4_H
@@ -27,6 +27,7 @@ extern "C" {
 #endif
 
 #define TN_INT4_MAX_FEATURES (1 << 21)
+#define TN_INT4_MAX_WEIGHTS (INT64_C(1) << 32)      /* of a tensor, with its sides rounded up to multiples of 64 (features) and 128 (the side that is summed over) */
 
 /* tn_int4_linear_desc.dtype, beside TN_DTYPE_F32 and TN_DTYPE_BF16: tensors that are in 4 bits already */
 #define TN_DTYPE_INT4 3
@@ -68,8 +69,9 @@ int tn_int4_linear_create(tn_int4_linear_t* out, const tn_int4_linear_desc* desc
 
 /*
  * Bytes of workspace that a call with `tokens` tokens needs (host only; negative: an error): for partial sums of products whose inputs are
- * split, and for rows that are laid out anew - where their length is no multiple of 128 (each segment's, of a transposed pair), where x is not
- * 16-byte aligned, or where x_stride is no multiple of 8 or 2^22 or more. gated: 1 for tn_int4_linear_gated.
+ * split, and for rows that are laid out anew - in fp16 for tiles; where the weight is streamed, if their length is no multiple of 128, x is not
+ * 16-byte aligned, or x_stride is no multiple of 8, or 2^22 or more. gated: 1 for tn_int4_linear_gated. The rows of the call itself must be no
+ * less aligned than the x that was asked for, with its x_stride.
  */
 int64_t tn_int4_linear_workspace(tn_int4_linear_t h, const void* x, int64_t x_stride, int64_t tokens, int32_t gated);
 
@@ -78,9 +80,11 @@ int64_t tn_int4_linear_workspace(tn_int4_linear_t h, const void* x, int64_t x_st
  * is [tokens, n_tensors * M], y is [tokens, N], the sum over the tensors of X_i W_i. y may not overlap x (TN_ERR_INVALID_ARG).
  * workspace: what the function above says, 256-byte aligned, for this call alone until its work is done: calls with workspaces of their own may be in
  * flight together. Nothing in it has to start at zero.
- * Rounding: up to 64 tokens (forward) products are taken with the codes as they are, which is exact, and sums are multiplied with the scales in fp32. Calls with
- * more, and transposed ones, round W to bf16 (half a unit: 2^-9 to 2^-8 of each weight; fp32 holds W exactly). A result that is not finite is what fp32 sums of
- * W[f][k] * x[k] are, apart from the order of the sum.
+ * Rounding. Up to 64 tokens (where tn_int4_linear_plan_query says that the weight is streamed) products are taken with the codes as they are, which is exact,
+ * and fp32 sums of a group are multiplied with its scale. In tiles, weights are rounded to fp16 under a power of two for each feature (with TN_FLAG_TRANSPOSE for each
+ * group of features): off by 2^-12 of themselves, or by 2^-35 of the largest scale of the feature (group) where that is more; and tokens are in fp16 under a power of two for
+ * each row, which is exact, or off by 2^-39 of the row's largest finite magnitude. Sums are fp32's (in the matrix cores). Infinities and NaN of a token show in its row alone, and as
+ * sums of W[f][k] * x[k] have them.
  */
 int tn_int4_linear_forward(tn_int4_linear_t h, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t tokens,
                            void* workspace, int64_t workspace_bytes, void* stream);

@@ -91,7 +91,8 @@ class AdamW:
     state_bits    32: m and v in fp32; 8: m and sqrt(v) in e4m3 with a scale for each 128 and rounding at random, 2.02 bytes a value instead of 8
     seed          of that rounding: whoever starts again from a state_dict() with the same seed gets the same results
 
-    A bfloat16 parameter is the rounding of an fp32 master held here, so that whoever sets it from outside calls reset_master().
+    A bfloat16 parameter is the rounding of an fp32 master held here, so that whoever sets it from outside calls reset_master(). Steps
+    of one optimizer follow each other (on one stream, or on several that wait for each other).
     """
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
@@ -106,6 +107,7 @@ class AdamW:
         self.params, self.lr, self.betas, self.eps, self.weight_decay = params, float(lr), (float(betas[0]), float(betas[1])), float(eps), decays
         self.state_bits, self.seed, self._gpu, self._device = int(state_bits), int(seed), gpu, device
         self._sizes, self._shapes = [p.numel() for p in params], [p.shape for p in params]
+        self._param_pointers = [p.data_ptr() for p in params]
         self._all_f32 = (ctypes.c_int32 * len(params))(*[TN_DTYPE_F32] * len(params))
         values = _state_values(self._sizes)
         kind = torch.float32 if state_bits == 32 else _CODES
@@ -196,6 +198,8 @@ class AdamW:
         all of them; norm: that norm where it is known already (gradient_norm's, or one over several ranks). Returns the norm, None without
         max_norm. Where it is not finite nothing changes."""
         pointers, codes = self._gradients(grads)
+        if [p.data_ptr() for p in self.params] != self._param_pointers:
+            raise RuntimeError("a parameter's memory is not where it was when the optimizer was made")
         rate, rate_ptr = self.lr, None
         if isinstance(lr, torch.Tensor):
             rate_ptr = self._scalar("lr", lr).data_ptr()

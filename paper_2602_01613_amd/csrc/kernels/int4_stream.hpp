@@ -39,16 +39,18 @@ __device__ __forceinline__ float sixteen_and_zero(unsigned s) { return __uint_as
 __device__ __forceinline__ float plain_sum(const unsigned* packed, const unsigned* words, const bf16_t* x, int k_blocks, int sub_shift, int block_step) {
     float sum = 0.f;
 #pragma unroll 1
-    for (int k = 0; k < k_blocks * kBlock; ++k) {
-        const int kb = k >> 7, in = k & 127;
+    for (int run = 0; run < k_blocks * 16; ++run) {          // 8 k: one word of codes, one scale
+        const int kb = run >> 4, in = (run & 15) * 8;
         const unsigned w = packed[int64_t(kb) * kPieceWords + ((in >> 3) & 3) * 64 + (in >> 5)];
         const unsigned s = words[kb * int64_t(block_step) + (in >> sub_shift) * kPiece];
-        sum += float(int(w >> element_bit(in & 7) & 15u) - int(s & 15u)) * word_scale(s) * float(x[k]);
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(x + int64_t(run) * 8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += float(int(w >> element_bit(e) & 15u) - int(s & 15u)) * word_scale(s) * float(v[e]);
     }
     return sum;
 }
 
-// (up to the sign of the exponent's last values: relative error 2^-21, and finite for every finite gate)
+// silu(gate) * up: relative error 2^-20, finite for every finite gate
 __device__ __forceinline__ float gated_value(float gate, float up) { return gate * sigmoid(gate) * up; }
 
 __device__ __forceinline__ bool is_finite(float v) { return (__float_as_uint(v) & 0x7fffffffu) < 0x7f800000u; }

@@ -54,7 +54,10 @@ int check_desc(const tn_int4_linear_desc& d) {
     if (d.group != 32 && d.group != 64 && d.group != 128) return TN_ERR_INVALID_ARG;
     if (d.dtype != TN_DTYPE_INT4 && d.dtype != TN_DTYPE_F32 && d.dtype != TN_DTYPE_BF16) return TN_ERR_INVALID_ARG;
     if (d.dtype == TN_DTYPE_INT4 && d.scale_dtype != TN_DTYPE_BF16 && d.scale_dtype != TN_DTYPE_F16) return TN_ERR_INVALID_ARG;
-    return d.out_features > TN_INT4_MAX_FEATURES || d.in_features > TN_INT4_MAX_FEATURES ? TN_ERR_UNSUPPORTED : TN_OK;
+    if (d.out_features > TN_INT4_MAX_FEATURES || d.in_features > TN_INT4_MAX_FEATURES) return TN_ERR_UNSUPPORTED;
+    // pieces of a tensor: offsets of its scale words within it are 32 bits, and launches that make it have fewer than 2^32 threads
+    const int64_t f = (d.flags & TN_FLAG_TRANSPOSE) ? d.in_features : d.out_features, k = (d.flags & TN_FLAG_TRANSPOSE) ? d.out_features : d.in_features;
+    return div_up(f, kFeaturePad) * (kFeaturePad / kPiece) * div_up(k, kBlock) > TN_INT4_MAX_WEIGHTS / (kPiece * kBlock) ? TN_ERR_UNSUPPORTED : TN_OK;
 }
 
 void lay_out(const tn_int4_linear_desc& d, tn_int4_linear_s& h) {

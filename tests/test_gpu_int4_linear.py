@@ -7,6 +7,7 @@ import torch
 import oracle.int4_oracle as I
 import paper_2602_01613_amd as tn
 from fp8_util import half_unit, host
+from int4_util import FORM_CASES
 
 pytestmark = pytest.mark.gpu
 
@@ -42,8 +43,8 @@ def bounds(made, group, x, exact_codes):
     """How far an fp32 sum may be from the 64-bit one, before its rounding to bf16, for each tensor [tokens, m].
 
     Streamed: products of 16 + code and of 16 + zero with x are exact, and every sum of n terms in fp32 is off by at most n * 2^-23 of the sum of their
-    magnitudes (2^-23, not 2^-24, as additions inside the matrix cores may cut off); n: a group's, the correction, the groups', the waves'. Otherwise each weight
-    is rounded to bf16, 2^-8 of it at the most, and k terms are summed."""
+    magnitudes (2^-23, not 2^-24, as additions inside the matrix cores may cut off); n: a group's, the correction, the groups', the waves'. In tiles each weight
+    is rounded to fp16, 2^-12 of it at the most (2^-11 here, for what is below fp16's normal range in these rows), and k terms are summed."""
     x = np.abs(host(x))
     result = []
     for c, s, z in made:
@@ -54,7 +55,7 @@ def bounds(made, group, x, exact_codes):
             result.append((group + 4 + k / group + 16) * 2.0 ** -23 * (x @ w.T))
         else:
             w = np.abs(I.weight(c, s.double().numpy(), z, group))
-            result.append((2.0 ** -8 + (k + 16) * 2.0 ** -23) * (x @ w.T))
+            result.append((2.0 ** -11 + (k + 16) * 2.0 ** -23) * (x @ w.T))
     return result
 
 
@@ -101,7 +102,7 @@ def test_input_gradient(tokens, m, n, group, zeros, scale, tensors):
     for i, w in enumerate(weights_of(made, group)):
         part = host(dy)[:, i * m:(i + 1) * m]
         ref, most = ref + part @ w, most + np.abs(part) @ np.abs(w)
-    check(dx, ref, (2.0 ** -8 + (tensors * m + 16) * 2.0 ** -23) * most)
+    check(dx, ref, (2.0 ** -11 + (tensors * m + 16) * 2.0 ** -23) * most)
 
 
 @pytest.mark.parametrize("tokens,m,n,group,zeros,scale,tensors", [c for c in CASES if c[1] * c[2] < 10 ** 7])
@@ -115,14 +116,54 @@ def test_gated(tokens, m, n, group, zeros, scale, tensors):
     check(layer.gated(x.cuda()), ref, 1.1 * og * (np.abs(up) + ou) + np.abs(gate) * ou + 2.0 ** -20 * (np.abs(ref) + 1e-30))
 
 
-def test_relative_error_is_that_of_roundings():
-    """Random weights: in the mean square a rounding to bf16 is 2^-8 / sqrt(12) of a step at most ... two of them (weights, output) stay below 2^-8."""
+@pytest.mark.parametrize("kind,tokens,m,n,group", FORM_CASES)
+def test_every_form(kind, tokens, m, n, group):
+    made = make(m, n, group, 2 if kind == "gated" else 1, tokens % 2 == 1, "f16" if m % 8 else "bf16", seed=tokens + m)
+    w = weights_of(made, group)
+    if kind == "back":
+        layer, dy = layer_of(made, n, group, tokens, transpose=True), rows(tokens, m, 4, 1e-3)
+        check(layer(dy.cuda()), host(dy) @ w[0], (2.0 ** -11 + (m + 16) * 2.0 ** -23) * (np.abs(host(dy)) @ np.abs(w[0])))
+        return
+    layer, x = layer_of(made, n, group, tokens), rows(tokens, n)
+    off = bounds(made, group, x, streamed(m, n, len(made), tokens, kind == "gated", group))
+    sums = [host(x) @ v.T for v in w]
+    if kind == "plain":
+        check(layer(x.cuda()), sums[0], off[0])
+    else:
+        ref = I.silu_gate(*sums)
+        check(layer.gated(x.cuda()), ref, 1.1 * off[0] * (np.abs(sums[1]) + off[1]) + np.abs(sums[0]) * off[1] + 2.0 ** -20 * (np.abs(ref) + 1e-30))
+
+
+def test_relative_error_is_that_of_one_rounding():
+    """Random weights and activations: a rounding to bf16 is off by 2^-9 of a value's power of two at the most and evenly spread, 2^-9 / sqrt(3) in the mean square of that, which
+    the values exceed: below 2^-9 / sqrt(3) of them. The weights' roundings to fp16, 2^-12, and the sums' add less than a tenth of it."""
     for tokens, transpose in ((8, False), (500, False), (500, True)):
         made = make(1024, 2048, 128, 1)
         layer, x = layer_of(made, 2048, 128, tokens, transpose=transpose), rows(tokens, 1024 if transpose else 2048)
         w = weights_of(made, 128)[0]
         ref = host(x) @ (w if transpose else w.T)
-        assert np.linalg.norm(host(layer(x.cuda())) - ref) <= 2.0 ** -8 * np.linalg.norm(ref)
+        assert np.linalg.norm(host(layer(x.cuda())) - ref) <= 1.1 * 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+def test_rows_and_scales_of_any_size_in_tiles(transpose):
+    """Tokens from 2^-120 to 2^120, one of zeros, one with channels 2^30 apart; features whose scales are 2^60 apart: each row and feature has its own power of two."""
+    m, n, tokens = 96, 512, 70
+    made = make(m, n, 128, 1)
+    codes, s, z = made[0]
+    grow = torch.exp2(torch.arange(m) % 60 - 30.0)[:, None] if not transpose else torch.exp2(torch.arange(4) * 20.0 - 40)[None, :]
+    made = [(codes, (s.float() * grow).bfloat16(), z)]
+    layer = layer_of(made, n, 128, tokens, transpose=transpose)
+    x = rows(tokens, m if transpose else n).float() * torch.exp2(torch.linspace(-120, 80, tokens).round())[:, None]
+    x[3] = 0
+    x[4, ::7] *= 2.0 ** 30
+    x = x.bfloat16()
+    w = weights_of(made, 128)[0]
+    w = w if transpose else w.T
+    most = np.abs(host(x)) @ np.abs(w) + w.shape[0] * 2.0 ** -35 * np.abs(host(x)).max(axis=1, keepdims=True) * np.abs(w).max(axis=0, keepdims=True)
+    y = layer(x.cuda())
+    check(y, host(x) @ w, (2.0 ** -11 + (w.shape[0] + 16) * 2.0 ** -23) * most + 2.0 ** -133)
+    assert bool((y[3] == 0).all())
 
 
 @pytest.mark.parametrize("tokens", [1, 20, 64, 65, 200])

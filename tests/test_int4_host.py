@@ -76,7 +76,8 @@ def _desc(**change):
     (dict(scale_dtype=0), INVALID), (dict(scale_dtype=2), INVALID), (dict(flags=2), INVALID), (dict(tensors=None), INVALID), (dict(tensors=[None]), INVALID),
     (dict(scales=None), INVALID), (dict(scales=[None]), INVALID), (dict(scales=[A + 1]), INVALID), (dict(zeros=[None]), INVALID),
     (dict(dtype=0, tensors=[A + 2]), INVALID), (dict(dtype=1, tensors=[A + 1]), INVALID), (dict(n_tensors=2, tensors=[A, None], scales=[A, A]), INVALID),
-    (dict(out_features=1 << 23), UNSUPPORTED), (dict(in_features=1 << 40), UNSUPPORTED)])
+    (dict(out_features=1 << 23), UNSUPPORTED), (dict(in_features=1 << 40), UNSUPPORTED), (dict(out_features=1 << 20, in_features=1 << 13), UNSUPPORTED),
+    (dict(out_features=1 << 13, in_features=1 << 20, flags=128), UNSUPPORTED)])
 def test_layer_descriptions_refused(change, status):
     h = ctypes.c_void_p(0)
     d, keep = _desc(**change)
@@ -140,3 +141,19 @@ def test_needs_a_gpu():
     if not torch.cuda.is_available():
         with pytest.raises(RuntimeError):
             tn.Int4Linear([torch.zeros(4, 4)], 1)
+
+
+TILES = (32, 64, 96, 128, 160, 192)
+
+
+def test_every_form_of_a_product_is_among_the_tested_sizes():
+    from int4_util import FORM_CASES
+    seen = set()
+    for kind, tokens, m, n, group in FORM_CASES:
+        ask = lambda what: tn.int4_plan_query(m, n, 2 if kind == "gated" else 1, tokens, kind == "gated", what, kind == "back", group)      # noqa: E731
+        tile, ranges, stream = ask(tn.TN_INT4_PLAN_TILE_TOKENS), ask(tn.TN_INT4_PLAN_RANGES), (ask(tn.TN_INT4_PLAN_STREAM_TOKENS), ask(tn.TN_INT4_PLAN_STREAM_PIECES))
+        assert (tile == 0) == (stream[0] > 0) == (stream[1] > 0) and (tile or ranges == 1)
+        seen.add((kind, tile, ranges > 1) if tile else (kind,) + stream)
+    want = {(k, t, s) for k in ("plain", "gated", "back") for t in TILES for s in (False, True)}
+    want |= {("plain", 16, 1), ("plain", 16, 2), ("plain", 16, 4), ("plain", 32, 4), ("gated", 16, 2), ("gated", 16, 4), ("gated", 32, 4)}
+    assert not want - seen, want - seen
