@@ -38,8 +38,14 @@ def quantize(v: np.ndarray, h16: np.ndarray):
     return (np.sign(np.asarray(v).reshape(-1, BLOCK)) * (below + up * step)).reshape(-1), e
 
 
-def step(p, g, m, v, t, lr, beta1, beta2, eps, decay, clip=1.0):
-    """(p, m, v) after step t."""
+def least_root(beta1: float, beta2: float) -> float:
+    """sqrt(v) / |m| at the least, over all pasts: m is a sum of (1 - beta1) beta1^i g_i, v one of (1 - beta2) beta2^i g_i^2."""
+    return ((1 - beta2) * (1 - beta1 ** 2 / beta2)) ** 0.5 / (1 - beta1) if beta1 ** 2 < beta2 else 0.0
+
+
+def step(p, g, m, v, t, lr, beta1, beta2, eps, decay, clip=1.0, least=0.0):
+    """(p, m, v) after step t; least: the root's least part of |m| (least_root, for states in 8 bits)."""
     g = g * clip
     m, v = beta1 * m + (1 - beta1) * g, beta2 * v + (1 - beta2) * g * g
-    return p * (1 - lr * decay) - lr * (m / (1 - beta1 ** t)) / (np.sqrt(v / (1 - beta2 ** t)) + eps), m, v
+    root = np.maximum(np.sqrt(v), least * np.abs(m))
+    return p * (1 - lr * decay) - lr * (m / (1 - beta1 ** t)) / (root / (1 - beta2 ** t) ** 0.5 + eps), m, v

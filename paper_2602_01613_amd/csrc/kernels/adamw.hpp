@@ -40,6 +40,7 @@ struct AdamwArgs {
     float* master;
     const StepScalars* scalars;
     float beta1, rest1, beta2, rest2, eps;
+    float least;                     // states in 8 bits: of |m|, what the root of v has at the least
 };
 
 // The part of a value of which a chunk of 8 is loaded as floats, whatever it is stored as
@@ -222,7 +223,11 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(AdamwArgs a, Gradients 
             m[q] = fmaf(a.beta1, m[q], a.rest1 * c);
             v[q] = fmaf(a.beta2, v[q], a.rest2 * c * c);
             root[q] = sqrtf(v[q]);
-            p[q] = fmaf(p[q], keep, -s.step * m[q] / fmaf(root[q], s.root_bias2, a.eps));
+            // A root that was rounded to zero beside an m that was not would move the parameter by m / eps: |m| <= sqrt(v) / least whatever the gradients were
+            // (Cauchy and Schwarz over their past), and a smaller root is a rounding. (A comparison: a NaN stays one.)
+            float under = root[q];
+            if constexpr (BITS == 8) under = under < a.least * fabsf(m[q]) ? a.least * fabsf(m[q]) : under;
+            p[q] = fmaf(p[q], keep, -s.step * m[q] / fmaf(under, s.root_bias2, a.eps));
         }
         if (n) {
             if (t.bf16) {

@@ -1,6 +1,7 @@
 // The AdamW step over many tensors (include/tn_adamw.h): host side and C ABI. Kernels: kernels/adamw.hpp.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <new>
 #include <vector>
@@ -62,6 +63,7 @@ AdamwArgs step_args(const tn_adamw_s& h) {
     a.rest1 = float(1 - h.beta1);
     a.beta2 = float(h.beta2);
     a.rest2 = float(1 - h.beta2);
+    a.least = h.beta1 * h.beta1 < h.beta2 ? float(std::sqrt((1 - h.beta2) * (1 - h.beta1 * h.beta1 / h.beta2)) / (1 - h.beta1)) : 0.f;
     a.eps = float(h.eps);
     return a;
 }

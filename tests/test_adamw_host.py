@@ -43,6 +43,22 @@ def test_rounding_is_right_on_average_and_to_a_neighbour():
     assert np.array_equal(O.quantize(-v, np.resize(h, v.size))[0], -codes)
 
 
+def test_roots_least_part_of_m_holds_for_every_past_and_is_reached():
+    rng = np.random.default_rng(0)
+    for beta1, beta2 in ((0.9, 0.999), (0.9, 0.95), (0.0, 0.9)):
+        least = O.least_root(beta1, beta2)
+        pasts = [np.ones(200), rng.standard_normal(200), (beta1 / beta2) ** np.arange(200)[::-1], np.eye(200)[150]]
+        parts = []
+        for past in pasts:
+            m = v = 0.0
+            for g in past:
+                _, m, v = O.step(0.0, g, m, v, 1, 0.0, beta1, beta2, 1.0, 0.0)
+                assert v ** 0.5 >= least * abs(m) * (1 - 1e-12)
+            parts.append(v ** 0.5 / max(abs(m), 1e-30))
+        assert abs(parts[2] / least - 1) < 1e-3            # the gradients that make the two sides alike
+    assert O.least_root(0.99, 0.9) == 0.0
+
+
 def test_hash_is_even_and_its_halves_and_steps_are_apart():
     """Means and correlations of 2^18 numbers, within five standard errors of what independent even ones have."""
     n = 1 << 18

@@ -80,7 +80,7 @@ class Setup:
 def check_step(s, before, states, t, got_states, clip=1.0, decay=DECAY, lr=LR):
     """fp32: a handful of roundings of 2^-24 for each of m, v and the parameter, the last one also with those of its move (hardware division and
     root: 2^-22), of which there are fewer than 16."""
-    p, m, v = O.step(before, s.flat(s.grads), *states, t, lr, *BETAS, EPS, decay, clip)
+    p, m, v = O.step(before, s.flat(s.grads), *states, t, lr, *BETAS, EPS, decay, clip, O.least_root(*BETAS) if s.bits == 8 else 0.0)
     g = np.abs(s.flat(s.grads)) * clip
     off_m = 2.0 ** -22 * (np.abs(states[0]) + g)
     off_v = 2.0 ** -21 * v
@@ -210,6 +210,23 @@ def test_states_in_8_bits_are_right_on_average():
     ratio_v = host(value("second") ** 2 / g ** 2) / (1 - 0.999 ** steps)
     assert abs(ratio_m.mean() - 1) < 5 * 2.0 ** -4 * 5.3 ** 0.5 / n ** 0.5
     assert -5 * 0.35 / n ** 0.5 < ratio_v.mean() - 1 < 1 / 14 + 5 * 0.35 / n ** 0.5
+
+
+def test_small_values_beside_large_ones_in_8_bits():
+    """In each block one gradient of 1 and others from 10^-5 to 10^-8, below the least codes: their m is now and then rounded to a code where the root is rounded to zero, and
+    later gradients are zero. No step is longer than lr * B * sqrt(1 - beta2^t) / (1 - beta1^t) <= lr * B * 1.01 (the last at t = 1: 0.32; beyond, less than one) and the root's fp32."""
+    n, steps = 1 << 14, 40
+    g = 10.0 ** -(5 + 3 * torch.rand(n, generator=torch.Generator().manual_seed(3)))
+    g[::128] = 1.0
+    g = g.cuda()
+    p = torch.zeros(n, device="cuda")
+    opt = tn.AdamW([p], lr=LR, betas=BETAS, weight_decay=0.0, state_bits=8, seed=9)
+    most = 0.0
+    for t in range(steps):
+        before = p.clone()
+        opt.step([g if t < 20 else torch.zeros_like(g)])
+        most = max(most, float((p - before).abs().max()))
+    assert most <= 1.01 * LR / O.least_root(*BETAS)
 
 
 @pytest.mark.parametrize("bits", [32, 8])
