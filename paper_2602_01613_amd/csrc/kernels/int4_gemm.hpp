@@ -82,12 +82,12 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    // XCD x takes a contiguous eighth of the tiles, in bands of a few rows of them (rows fastest): what runs there at a time shares
+    // XCD x takes a contiguous eighth of the tiles, in bands of a few rows of them (rows fastest, ranges of k slowest): what runs there at a time shares
     // panels of both operands in its L2
     const int n_items = g.n_row * g.n_col * a.n_split, xcd = blockIdx.x & 7;
     const int item = int(int64_t(n_items) * xcd >> 3) + int(blockIdx.x >> 3);
     if (item >= int(int64_t(n_items) * (xcd + 1) >> 3)) return;
-    const int tile = item / a.n_split, split = __builtin_amdgcn_readfirstlane(item - tile * a.n_split);
+    const int split = __builtin_amdgcn_readfirstlane(item / (g.n_row * g.n_col)), tile = item - split * (g.n_row * g.n_col);
     const int band = tile / (g.band * g.n_col), in_band = tile - band * (g.band * g.n_col);
     const int band_rows = min(g.band, g.n_row - band * g.band);
     const int col_tile = __builtin_amdgcn_readfirstlane(in_band / band_rows);
@@ -294,7 +294,7 @@ __device__ __forceinline__ void int4_tile(const Int4GemmArgs& g) {
     for (int i = 0; i < TM; ++i) {
         const int64_t token = row0 + i * 16 + r;
         if (token >= a.tokens) continue;
-        const int e = a.x_exponents[token];
+        const int e = a.x_exponents[FORM == INT4_PARTIAL ? int64_t(split) * a.tokens + token : token];
 #pragma unroll
         for (int f = 0; f < 4; ++f)
 #pragma unroll

@@ -174,13 +174,14 @@ __global__ void __launch_bounds__(256) int4_rows_kernel(const bf16_t* x, int64_t
 }
 
 // The same rows in fp16 for the tiles, each divided by the power of two that puts its largest finite magnitude into [2^14, 2^15): exact but below 2^-29 of
-// that, and there off by 2^-40 of it at most. A workgroup takes a row; NC chunks of it stay in a thread's registers between the maximum and
-// the conversion, longer rows are read again from the caches.
+// that, and there off by 2^-40 of it at most. A workgroup takes a row, or where the inputs are split a range of one, which has its own power of two (77 rows of 51200 are
+// 12 ranges each: 20 us as whole rows, on 77 CUs, 6 so); NC chunks of it stay in a thread's registers between the maximum and
+// the conversion, what is longer is read again from the caches.
 template <int NC>
-__global__ void __launch_bounds__(256) int4_half_rows_kernel(const bf16_t* x, int64_t x_stride, int32_t segments, int64_t cols, int64_t padded, _Float16* out,
-                                                             int32_t* exponents) {
+__global__ void __launch_bounds__(256) int4_half_rows_kernel(const bf16_t* x, int64_t x_stride, int32_t segments, int64_t cols, int64_t padded, int64_t range, _Float16* out,
+                                                             int32_t* exponents, int64_t exponents_stride) {
     __shared__ unsigned part[4];
-    const int64_t token = blockIdx.x, chunks = segments * padded / kChunk;
+    const int64_t token = blockIdx.x, first = blockIdx.y * range, all = segments * padded / kChunk, chunks = first + range < all ? first + range : all;
     x += token * x_stride;
     out += token * segments * padded;
     auto load = [&](int64_t i) {
@@ -196,13 +197,13 @@ __global__ void __launch_bounds__(256) int4_half_rows_kernel(const bf16_t* x, in
     Chunk<bf16_t> held[NC];
 #pragma unroll
     for (int h = 0; h < NC; ++h) {
-        const int64_t i = h * 256 + int(threadIdx.x);
+        const int64_t i = first + h * 256 + int(threadIdx.x);
         if (i < chunks) held[h] = load(i);
     }
 #pragma unroll
     for (int h = 0; h < NC; ++h)
-        if (h * 256 + int(threadIdx.x) < chunks) look(held[h]);
-    for (int64_t i = NC * 256 + threadIdx.x; i < chunks; i += 256) look(load(i));
+        if (first + h * 256 + int(threadIdx.x) < chunks) look(held[h]);
+    for (int64_t i = first + NC * 256 + threadIdx.x; i < chunks; i += 256) look(load(i));
     most = row16_max(most);
     most = max(most, unsigned(__shfl_xor(int(most), 16)));
     most = max(most, unsigned(__shfl_xor(int(most), 32)));
@@ -224,7 +225,7 @@ __global__ void __launch_bounds__(256) int4_half_rows_kernel(const bf16_t* x, in
     };
 #pragma unroll
     for (int h = 0; h < NC; ++h)
-        if (h * 256 + int(threadIdx.x) < chunks) store(held[h], h * 256 + int(threadIdx.x));
-    for (int64_t i = NC * 256 + threadIdx.x; i < chunks; i += 256) store(load(i), i);
-    if (threadIdx.x == 0) exponents[token] = e;
+        if (first + h * 256 + int(threadIdx.x) < chunks) store(held[h], first + h * 256 + int(threadIdx.x));
+    for (int64_t i = first + NC * 256 + threadIdx.x; i < chunks; i += 256) store(load(i), i);
+    if (threadIdx.x == 0) exponents[blockIdx.y * exponents_stride + token] = e;
 }

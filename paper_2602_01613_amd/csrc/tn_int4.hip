@@ -242,11 +242,10 @@ int gemm_form(const Int4GemmArgs& g, hipStream_t stream) {
     return g.l.sub == 1 ? run_gemm<TM, FORM, false, 1>(g, stream) : g.l.sub == 2 ? run_gemm<TM, FORM, false, 2>(g, stream) : run_gemm<TM, FORM, false, 4>(g, stream);
 }
 template <int TM>
-int run_tiles(const Int4Args& a, bool gated, hipStream_t stream) {
+int run_tiles(const Int4Args& a, int64_t range, bool gated, hipStream_t stream) {
     Int4GemmArgs g{};
     g.l = a;
-    g.blocks_per_split = int(div_up(a.k_blocks, a.n_split));
-    g.l.n_split = int(div_up(a.k_blocks, g.blocks_per_split));         // no range without a block
+    g.blocks_per_split = int(range);
     const bool fused = gated && !a.partial;
     const int64_t pieces = int64_t(a.f_pieces) * a.tensors;
     const int64_t n_row = div_up(a.tokens, 16 * TM), n_col = fused ? div_up(a.f_pieces, 8) : div_up(pieces, 16);
@@ -287,21 +286,21 @@ struct Workspace {
 Workspace workspace_of(const tn_int4_linear_s& h, const Int4Args& a, const Choice& c) {
     Workspace w;
     if (c.tm || laid_out_anew(h, a.x, a.x_stride)) w.rows = whole(a.tokens * h.k_blocks * kBlock * 2);
-    if (c.tm) w.exponents = whole(a.tokens * 4);
+    if (c.tm) w.exponents = whole(c.split * a.tokens * 4);
     if (c.tm && c.split > 1) w.sums = whole(c.split * a.tokens * a.ld * 4);
     return w;
 }
 
-int half_rows(const tn_int4_linear_s& h, const Int4Args& a, _Float16* rows, int32_t* exponents, hipStream_t stream) {
+int half_rows(const tn_int4_linear_s& h, const Int4Args& a, int ranges, int64_t blocks, _Float16* rows, int32_t* exponents, hipStream_t stream) {
     const bf16_t* x = static_cast<const bf16_t*>(a.x);
-    const int64_t padded = h.own_k_blocks * kBlock, chunks = h.k_blocks * (kBlock / kChunk), run = int64_t(1) << 22;
+    const int64_t padded = h.own_k_blocks * kBlock, chunks = blocks * (kBlock / kChunk), run = int64_t(1) << 19;
     for (int64_t at = 0; at < a.tokens; at += run) {              // a launch has fewer than 2^32 threads
-        const dim3 grid(unsigned(a.tokens - at < run ? a.tokens - at : run));
+        const dim3 grid(unsigned(a.tokens - at < run ? a.tokens - at : run), unsigned(ranges));
         const bf16_t* from = x + at * a.x_stride;
         _Float16* to = rows + at * h.k_blocks * kBlock;
-        if (chunks <= 512) int4_half_rows_kernel<2><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, to, exponents + at);
-        else if (chunks <= 1024) int4_half_rows_kernel<4><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, to, exponents + at);
-        else int4_half_rows_kernel<13><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, to, exponents + at);
+        if (chunks <= 512) int4_half_rows_kernel<2><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, chunks, to, exponents + at, a.tokens);
+        else if (chunks <= 1024) int4_half_rows_kernel<4><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, chunks, to, exponents + at, a.tokens);
+        else int4_half_rows_kernel<13><<<grid, dim3(256), 0, stream>>>(from, a.x_stride, h.k_segments, h.k_cols, padded, chunks, to, exponents + at, a.tokens);
         const int rc = launched();
         if (rc != TN_OK) return rc;
     }
@@ -323,11 +322,13 @@ int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void
     if (w.all() > 0 && (!workspace || workspace_bytes < w.all() || !aligned(workspace, 256))) return TN_ERR_INVALID_ARG;
     a.y = static_cast<bf16_t*>(y);
     a.y_stride = y_stride;
+    const int64_t range = div_up(a.k_blocks, c.split);
+    a.n_split = int32_t(div_up(a.k_blocks, range));         // no range without a block
     if (w.rows) {
         int rc;
         if (c.tm) {
             int32_t* exponents = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + w.rows);
-            rc = half_rows(h, a, static_cast<_Float16*>(workspace), exponents, stream);
+            rc = half_rows(h, a, a.n_split, range, static_cast<_Float16*>(workspace), exponents, stream);
             a.x_exponents = exponents;
         } else {
             const int64_t blocks = div_up(tokens * h.k_blocks * (kBlock / kChunk), 256);
@@ -340,15 +341,14 @@ int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void
         a.x_stride = h.k_blocks * kBlock;
     }
     if (c.tm == 0) return a.sub == 1 ? stream_sizes<1>(a, c, gated, stream) : a.sub == 2 ? stream_sizes<2>(a, c, gated, stream) : stream_sizes<4>(a, c, gated, stream);
-    a.n_split = c.split;
     if (c.split > 1) a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.rows + w.exponents);
     switch (c.tm) {
-        case 2: return run_tiles<2>(a, gated, stream);
-        case 4: return run_tiles<4>(a, gated, stream);
-        case 6: return run_tiles<6>(a, gated, stream);
-        case 8: return run_tiles<8>(a, gated, stream);
-        case 10: return run_tiles<10>(a, gated, stream);
-        default: return run_tiles<12>(a, gated, stream);
+        case 2: return run_tiles<2>(a, range, gated, stream);
+        case 4: return run_tiles<4>(a, range, gated, stream);
+        case 6: return run_tiles<6>(a, range, gated, stream);
+        case 8: return run_tiles<8>(a, range, gated, stream);
+        case 10: return run_tiles<10>(a, range, gated, stream);
+        default: return run_tiles<12>(a, range, gated, stream);
     }
 }
 
