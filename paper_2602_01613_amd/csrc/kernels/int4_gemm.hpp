@@ -14,6 +14,11 @@
 // A step is 32 k: 4 * TM MFMAs, tokens outermost. Behind the four of token fragment i the fragment that the next step has in its place is
 // read into the same registers. A stage is two steps; what the first one reads (its second half) are the last reads of the stage, so that after the
 // barrier in the second step the stage after next but one goes where it is.
+//
+// Measured: 8192 x 5120 -> 25600 in 1745 us, 1.23 PFLOP/s (the vendor library's bf16 product of the same sizes 1775), matrix cores busy 56 % of the cycles at 2.1 GHz; 77 x
+// 51200 -> 5120 (transposed) 62 us, busy 32 %. What bounds it is the one wave of each SIMD: its conversions (60 instructions of four cycles a step) hide only in part behind 4 * TM MFMAs of 16, so that
+// a step takes about 140 ns more than its MFMAs at any TM, and large tiles are best wherever they fill the chip. More stages of tokens in LDS (four to six), and codes and
+// scale words read a step ahead of their use, changed nothing (1 %).
 // ---------------------------------------------------------------------------------------------
 enum Int4Form : int { INT4_PLAIN = 0, INT4_GATED = 1, INT4_PARTIAL = 2 };
 

@@ -17,7 +17,7 @@ namespace {
 static_assert(TN_ADAMW_BLOCK == kBlock, "states share the 8-bit format of rows");
 
 constexpr int64_t kMostValues = int64_t(1) << 40;
-constexpr int kNormGroups = 2048;                // workgroups of the norm, over all its launches
+constexpr int kNormGroups = 2048, kNormSums = 8192;      // workgroups of a launch of the norm, and of all of them (one each at the least)
 constexpr int64_t kLaunchParts = int64_t(1) << 22;
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -98,12 +98,13 @@ int for_launches(const tn_adamw_s& h, const void* const* grads, const int32_t* d
     return rc;
 }
 
-// Workgroups of the norm's launch over these parts: its share of kNormGroups, rounded up
-int64_t norm_groups(const tn_adamw_s& h, int64_t parts) {
-    const int64_t all = h.part0.back(), share = div_up(parts * kNormGroups, all > kNormGroups ? all : kNormGroups);
-    return share < 1 ? 1 : share;
-}
 int64_t norm_launches(const tn_adamw_s& h) { return div_up(h.n_tensors, kLaunchTensors) + h.part0.back() / kLaunchParts; }
+// Workgroups of a launch of the norm over these parts, as many as it has room for: launches follow each other, so that a short one is as long as what one workgroup
+// does (1604 parts behind 27392 others: 16 us as a share of 2048 workgroups, 8 so)
+int64_t norm_groups(const tn_adamw_s& h, int64_t parts) {
+    const int64_t room = kNormSums / norm_launches(h), most = room < 1 ? 1 : room < kNormGroups ? room : kNormGroups;
+    return parts < most ? parts : most;
+}
 
 int run_norm(const tn_adamw_s& h, const void* const* grads, const int32_t* dtypes, double* sums, int32_t* n_sums, hipStream_t stream) {
     int64_t done = 0;
@@ -205,7 +206,7 @@ int tn_adamw_create(tn_adamw_t* out, const tn_adamw_desc* d) {
 
 int64_t tn_adamw_workspace(tn_adamw_t h) {
     if (!h) return TN_ERR_INVALID_ARG;
-    return (kNormGroups + norm_launches(*h)) * int64_t(sizeof(double));
+    return (kNormSums + norm_launches(*h)) * int64_t(sizeof(double));
 }
 
 int tn_adamw_gradient_norm(tn_adamw_t h, const void* const* grads, const int32_t* grad_dtypes, float* norm, void* workspace, int64_t workspace_bytes, void* stream) {

@@ -127,7 +127,8 @@ Int4Args product_args(const tn_int4_linear_s& h, const void* x, int64_t x_stride
 // ---------------------------------------------------------------------------------------------
 // which kernel a product runs on
 // ---------------------------------------------------------------------------------------------
-// Times in us, fitted to measurements on the MI355X (256 CUs) of products of 5120 to 51200 inputs and 1024 to 51200 outputs, 1 to 8192 tokens.
+// Times in us, fitted to measurements on the MI355X (256 CUs) of products of 5120 to 51200 inputs and 1024 to 51200 outputs, 1 to 8192 tokens. Of the forms measured at such
+// sizes the one chosen is mostly within 3 % of the best, and 1.1 times it at the worst.
 constexpr int64_t kStreamTokens = 64;           // streamed up to here at the most
 struct TileCost {
     int tm, per_cu;
