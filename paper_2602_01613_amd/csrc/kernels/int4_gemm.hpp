@@ -5,8 +5,8 @@
 // ---------------------------------------------------------------------------------------------
 // A workgroup of four waves computes 16 * TM tokens x 256 features: each wave all of the tokens x 64 features, in TM x 4 accumulators of
 // v_mfma_f32_16x16x32_f16. Side by side along the features, no two waves make the same weight: its codes go from memory to registers in the
-// operand's order (1 KB a load) and become fp16 there, (code - zero) * (scale / 2^e) with one rounding of 2^-12; two weights are a shift, a mask, an or, an addition
-// and a multiplication of packed halves, dealt out between the MFMAs of the step before. (In bf16 the rounding was 2^-9, as large as the output's, and the
+// operand's order (1 KB a load) and become fp16 there, (code - zero) * (scale / 2^e) with one rounding of 2^-11; two weights are a shift, a mask, an or, an addition
+// and a multiplication of packed halves, dealt out between the MFMAs of the step before. (In bf16 the rounding was 2^-8, as large as the output's, and the
 // conversion half as long again.) The tokens, in fp16 under a power of two for each row, go from memory to LDS without passing through registers, in three stages
 // of 64 k; a row is 128 bytes there, its 16-byte chunk c at position c ^ ((row / 2) % 8), so that the 16 rows a read touches at a time fall on 16
 // different slots of the 64 banks.

@@ -76,7 +76,7 @@ __device__ __forceinline__ void store4(bf16_t* p, int n, floatx4 v) {
 // tokens, and all of k, which its waves deal out block by block and add up through LDS in a fixed order. Each wave has RING blocks requested ahead.
 //
 // Bound by HBM for one token: 5120 -> 2 x 25600 gated 31 us, 136 MB at 4.4 TB/s; 5120 -> 8192 7.1 us. With more tokens by their reads, which every workgroup makes anew and
-// which come at 5 to 6 TB/s over all of them: 25600 -> 5120 with 8 tokens 24 us, 70 MB of weights and as much of tokens.
+// which come at 5 to 6 TB/s over all of them: 25600 -> 5120 with 8 tokens 24 us, 74 MB of weights and 65 of tokens.
 // ---------------------------------------------------------------------------------------------
 template <int GROUPS, int TG, int SUB>
 struct StreamBlock {

@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) int4_rows_kernel(const bf16_t* x, int64_t
 }
 
 // The same rows in fp16 for the tiles, each divided by the power of two that puts its largest finite magnitude into [2^14, 2^15): exact but below 2^-29 of
-// that, and there off by 2^-40 of it at most. A workgroup takes a row, or where the inputs are split a range of one, which has its own power of two (77 rows of 51200 are
+// that, and there off by 2^-39 of it at most. A workgroup takes a row, or where the inputs are split a range of one, which has its own power of two (77 rows of 51200 are
 // 12 ranges each: 20 us as whole rows, on 77 CUs, 6 so); NC chunks of it stay in a thread's registers between the maximum and
 // the conversion, what is longer is read again from the caches.
 template <int NC>

@@ -44,7 +44,7 @@ def bounds(made, group, x, exact_codes):
 
     Streamed: products of 16 + code and of 16 + zero with x are exact, and every sum of n terms in fp32 is off by at most n * 2^-23 of the sum of their
     magnitudes (2^-23, not 2^-24, as additions inside the matrix cores may cut off); n: a group's, the correction, the groups', the waves'. In tiles each weight
-    is rounded to fp16, 2^-12 of it at the most (2^-11 here, for what is below fp16's normal range in these rows), and k terms are summed."""
+    is rounded to fp16, 2^-11 of it at the most, and k terms are summed."""
     x = np.abs(host(x))
     result = []
     for c, s, z in made:
@@ -135,8 +135,8 @@ def test_every_form(kind, tokens, m, n, group):
 
 
 def test_relative_error_is_that_of_one_rounding():
-    """Random weights and activations: a rounding to bf16 is off by 2^-9 of a value's power of two at the most and evenly spread, 2^-9 / sqrt(3) in the mean square of that, which
-    the values exceed: below 2^-9 / sqrt(3) of them. The weights' roundings to fp16, 2^-12, and the sums' add less than a tenth of it."""
+    """Random weights and activations: a rounding to bf16 is off by 2^-8 of a value's power of two at the most and evenly spread, 2^-8 / sqrt(3) in the mean square of that, which
+    the values exceed: below 2^-8 / sqrt(3) of them. The weights' roundings to fp16, 2^-11, and the sums' add less than a tenth of it."""
     for tokens, transpose in ((8, False), (500, False), (500, True)):
         made = make(1024, 2048, 128, 1)
         layer, x = layer_of(made, 2048, 128, tokens, transpose=transpose), rows(tokens, 1024 if transpose else 2048)
