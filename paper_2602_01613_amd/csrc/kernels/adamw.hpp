@@ -234,13 +234,9 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(AdamwArgs a, Gradients 
 #pragma unroll
         for (int q = 0; q < kChunk; ++q) {
             const float c = g[q] * s.clip;
-            if constexpr (BITS == 32) {
-                m[q] = fmaf(a.beta1, m[q], a.rest1 * c);
-                v[q] = fmaf(a.beta2, v[q], a.rest2 * c * c);
-            } else {
-                m[q] = weighted(a.beta1, m[q], a.rest1, c);
-                v[q] = fmaf(a.rest2, fmaf(c, c, -v[q]), v[q]);
-            }
+            m[q] = BITS == 32 ? fmaf(a.beta1, m[q], a.rest1 * c) : weighted(a.beta1, m[q], a.rest1, c);
+            if (BITS == 8 && a.beta2 >= 0.5f) v[q] = fmaf(a.rest2, fmaf(c, c, -v[q]), v[q]);          // (with less of v left, its rounding would be larger than c^2)
+            else v[q] = fmaf(a.beta2, v[q], a.rest2 * c * c);
             root[q] = sqrtf(v[q]);
             // A root that was rounded to zero beside an m that was not would move the parameter by m / eps: |m| <= sqrt(v) / least whatever the gradients were
             // (Cauchy and Schwarz over their past), and a smaller root is a rounding. (A comparison: a NaN stays one.)

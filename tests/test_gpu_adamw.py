@@ -230,6 +230,17 @@ def test_small_values_beside_large_ones_in_8_bits():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_states_that_forget_all(bits):
+    """betas of 0: each step is lr * g / (|g| + eps), whatever came before; g, then 10^-5 of it. (fp32: a few roundings of the move, and of the parameter, 2^-24 * 2 lr.)"""
+    p = torch.zeros(300, device="cuda")
+    opt = tn.AdamW([p], lr=LR, betas=(0.0, 0.0), eps=EPS, weight_decay=0.0, state_bits=bits)
+    for g in (1.0, 1e-5, -0.25):
+        before = host(p)
+        opt.step([torch.full((300,), g, device="cuda")])
+        assert np.abs((host(p) - before) / LR + g / (abs(g) + EPS)).max() <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_same_from_run_to_run_and_from_a_saved_state(bits):
     a, b = (Setup(SIZES, "mixed", "mixed", bits, seed=2) for _ in range(2))
     for _ in range(3):
