@@ -106,7 +106,11 @@ int tn_adamw_gradient_norm(tn_adamw_t h, const void* const* grads, const int32_t
 int tn_adamw_step(tn_adamw_t h, const void* const* grads, const int32_t* grad_dtypes, double lr, const float* lr_device, double max_norm, float* norm,
                   int32_t norm_given, void* workspace, int64_t workspace_bytes, void* stream);
 
-/* No call may be in flight. NULL is accepted. */
+/* Masters of the parameters in bf16 from the parameters as they are: for whoever sets a parameter from outside. The handle stays as it is, so that captured steps
+ * are replayed as before; where no parameter is in bf16 there is nothing to do. It is one of the handle's steps: none of them may overlap it in time. */
+int tn_adamw_reset_master(tn_adamw_t h, void* stream);
+
+/* No call may be in flight, and no graph that captured one may be replayed afterwards: its kernels read the handle's memory. NULL is accepted. */
 int tn_adamw_destroy(tn_adamw_t h);
 
 #ifdef __cplusplus

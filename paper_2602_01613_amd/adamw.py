@@ -25,6 +25,7 @@ ADAMW_EXPORTED_SYMBOLS = (
     "tn_adamw_workspace",
     "tn_adamw_gradient_norm",
     "tn_adamw_step",
+    "tn_adamw_reset_master",
     "tn_adamw_destroy",
 )
 
@@ -66,6 +67,7 @@ def _library():
             "tn_adamw_workspace": [p],
             "tn_adamw_gradient_norm": [p, ctypes.POINTER(p), ctypes.POINTER(i32), p, p, i64, p],
             "tn_adamw_step": [p, ctypes.POINTER(p), ctypes.POINTER(i32), f64, p, f64, p, i32, p, i64, p],
+            "tn_adamw_reset_master": [p, p],
             "tn_adamw_destroy": [p],
         }
         for name, types in args.items():
@@ -92,7 +94,7 @@ class AdamW:
     seed          of that rounding: whoever starts again from a state_dict() with the same seed gets the same results
 
     A bfloat16 parameter is the rounding of an fp32 master held here, so that whoever sets it from outside calls reset_master(). Steps
-    of one optimizer follow each other (on one stream, or on several that wait for each other).
+    of one optimizer follow each other (on one stream, or on several that wait for each other). Graphs that captured them are not replayed after close().
     """
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
@@ -117,9 +119,9 @@ class AdamW:
             self._state["first_scales"], self._state["second_scales"] = new(values // TN_ADAMW_BLOCK, _SCALES), new(values // TN_ADAMW_BLOCK, _SCALES)
         if any(p.dtype == torch.bfloat16 for p in params):
             self._state["master"] = new(values, torch.float32)
-        self._make(True)
+        self._make()
 
-    def _make(self, init_master: bool) -> None:
+    def _make(self) -> None:
         n, s = len(self.params), self._state
         desc = _Desc()
         desc.n_tensors, desc.state_bits = n, self.state_bits
@@ -132,7 +134,7 @@ class AdamW:
             desc.first_scales, desc.second_scales = s["first_scales"].data_ptr(), s["second_scales"].data_ptr()
         if "master" in s:
             desc.master = s["master"].data_ptr()
-        desc.beta1, desc.beta2, desc.eps, desc.seed, desc.init_master = *self.betas, self.eps, self.seed, int(init_master)
+        desc.beta1, desc.beta2, desc.eps, desc.seed, desc.init_master = *self.betas, self.eps, self.seed, 1
         desc.stream = _stream(self._gpu)
         h = ctypes.c_void_p(0)
         _check(_library().tn_adamw_create(ctypes.byref(h), ctypes.byref(desc)), "tn_adamw_create")
@@ -140,10 +142,10 @@ class AdamW:
         self._workspace_bytes = int(_lib.tn_adamw_workspace(self._handle))
 
     def reset_master(self) -> None:
-        """Masters from the parameters as they are (waits for the GPU; not while a graph is captured)."""
+        """Masters from the parameters as they are: one launch on the current stream, in its place among the steps. Captured steps stay
+        valid, and read the new masters."""
         self._open()
-        self.close()
-        self._make(True)
+        _check(_lib.tn_adamw_reset_master(self._handle, _stream(self._gpu)), "tn_adamw_reset_master")
 
     def _open(self) -> None:
         if self._handle is None:

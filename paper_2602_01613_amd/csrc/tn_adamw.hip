@@ -30,6 +30,7 @@ unsigned type_bytes(int32_t t) { return t == TN_DTYPE_F32 ? 4 : 2; }
 
 struct tn_adamw_s {
     int32_t n_tensors = 0, bits = 32;
+    bool masters = false;                        // some parameter is in bf16
     std::vector<int64_t> sizes, part0;           // part0[i]: first part of tensor i; part0[n]: all parts
     TensorEntry* tensors = nullptr;              // device
     PartEntry* parts = nullptr;
@@ -117,6 +118,16 @@ int run_norm(const tn_adamw_s& h, const void* const* grads, const int32_t* dtype
     *n_sums = int32_t(done);
     return rc;
 }
+
+int make_masters(const tn_adamw_s& h, hipStream_t stream) {
+    if (!h.masters) return TN_OK;
+    AdamwArgs a = step_args(h);
+    a.n_parts = h.part0.back();
+    const int64_t groups = a.n_parts < 4096 ? a.n_parts : 4096;
+    adamw_master_kernel<<<dim3(unsigned(groups)), dim3(256), 0, stream>>>(a);
+    return launched();
+}
+
 bool workspace_ok(tn_adamw_t h, const void* p, int64_t bytes) { return p && bytes >= tn_adamw_workspace(h) && aligned(p, 256); }
 
 }  // namespace
@@ -173,6 +184,7 @@ int tn_adamw_create(tn_adamw_t* out, const tn_adamw_desc* d) {
     h->first_scales = static_cast<unsigned char*>(d->first_scales);
     h->second_scales = static_cast<unsigned char*>(d->second_scales);
     h->master = d->master;
+    h->masters = masters;
     h->count = d->count;
     h->beta1 = d->beta1;
     h->beta2 = d->beta2;
@@ -188,13 +200,7 @@ int tn_adamw_create(tn_adamw_t* out, const tn_adamw_desc* d) {
     if (rc == TN_OK && (hipMemcpyAsync(h->tensors, tensors.data(), tensors.size() * sizeof(TensorEntry), hipMemcpyHostToDevice, st) != hipSuccess ||
                         (!parts.empty() && hipMemcpyAsync(h->parts, parts.data(), parts.size() * sizeof(PartEntry), hipMemcpyHostToDevice, st) != hipSuccess)))
         rc = TN_ERR_HIP;
-    if (rc == TN_OK && masters && d->init_master) {
-        AdamwArgs a = step_args(*h);
-        a.n_parts = int64_t(parts.size());
-        const int64_t groups = a.n_parts < 4096 ? a.n_parts : 4096;
-        adamw_master_kernel<<<dim3(unsigned(groups)), dim3(256), 0, st>>>(a);
-        rc = launched();
-    }
+    if (rc == TN_OK && d->init_master) rc = make_masters(*h, st);
     if (hipStreamSynchronize(st) != hipSuccess && rc == TN_OK) rc = TN_ERR_HIP;       // (the host's arrays go out of scope)
     if (rc != TN_OK) {
         delete h;
@@ -255,6 +261,11 @@ int tn_adamw_step(tn_adamw_t h, const void* const* grads, const int32_t* grad_dt
         else adamw_step_kernel<8><<<grid, dim3(256), 0, st>>>(a, g);
         return launched();
     });
+}
+
+int tn_adamw_reset_master(tn_adamw_t h, void* stream) {
+    if (!h) return TN_ERR_INVALID_ARG;
+    return make_masters(*h, static_cast<hipStream_t>(stream));
 }
 
 int tn_adamw_destroy(tn_adamw_t h) {

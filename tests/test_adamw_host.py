@@ -159,3 +159,84 @@ def test_needs_a_gpu():
     if not torch.cuda.is_available():
         with pytest.raises(RuntimeError):
             tn.AdamW([torch.zeros(4)])
+
+
+class _Recorder:
+    """A library whose functions note their calls and succeed."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name,) + args) or 0
+
+
+def _optimizer(monkeypatch, params, **more):
+    """(an optimizer of these tensors, which say that they are on GPU 0, its library's calls)"""
+    lib = _Recorder()
+    monkeypatch.setattr(fp8, "_current_gpu", lambda: 0)
+    for name, value in (("_lib", lib), ("_library", lambda: lib), ("_stream", lambda gpu: 99)):
+        monkeypatch.setattr(adamw, name, value)
+    opt = tn.AdamW.__new__(tn.AdamW)
+    state = {"first": torch.zeros(128), "second": torch.zeros(128), "count": torch.zeros((), dtype=torch.int64), "master": torch.zeros(128)}
+    fields = dict(_handle=123, _gpu=0, params=params, lr=0.1, betas=(0.9, 0.99), eps=1e-8, weight_decay=[0.0] * len(params), state_bits=32, seed=0, _state=state,
+                  _sizes=[p.numel() for p in params], _shapes=[p.shape for p in params], _param_pointers=[p.data_ptr() for p in params],
+                  _all_f32=(ctypes.c_int32 * len(params))(), _workspace_bytes=256, _device="cpu")
+    for name, value in {**fields, **more}.items():
+        setattr(opt, name, value)
+    return opt, lib.calls
+
+
+def test_reset_master_keeps_the_handle(monkeypatch):
+    """Captured steps have the addresses of the handle's tables: it is neither destroyed nor made anew."""
+    from fp8_util import on_gpu
+    opt, calls = _optimizer(monkeypatch, [on_gpu(torch.zeros(5, dtype=torch.bfloat16), 0)])
+    opt.reset_master()
+    assert calls == [("tn_adamw_reset_master", 123, 99)] and opt._handle == 123
+    opt.close()
+    with pytest.raises(RuntimeError):
+        opt.reset_master()
+
+
+def test_reset_master_refuses_no_handle():
+    assert adamw._library().tn_adamw_reset_master(None, None) == INVALID
+
+
+RESET = """
+import ctypes, json, os
+import paper_2602_01613_amd as tn
+from paper_2602_01613_amd import adamw
+import test_adamw_host as host
+lib = adamw._library()
+hip = ctypes.CDLL(os.environ['LD_PRELOAD'])
+hip.fake_hip_take_launches.restype = ctypes.c_char_p
+take = lambda: [l.split()[0] for l in hip.fake_hip_take_launches().decode().splitlines()]
+mem = ctypes.create_string_buffer(65536)
+at = (ctypes.addressof(mem) + 255) // 256 * 256
+found = []
+for dtypes, sizes in (([0, 1], [5, 6]), ([0, 0], [5, 6]), ([0, 1], [5, 0])):
+    d, keep = host._desc(dtypes=dtypes, sizes=sizes, params=[at, at + 256], first=at, second=at, first_scales=at, second_scales=at, master=at, count=at, init_master=0)
+    h = ctypes.c_void_p(0)
+    assert lib.tn_adamw_create(ctypes.byref(h), ctypes.byref(d)) == 0
+    made = take()
+    assert lib.tn_adamw_reset_master(h, None) == 0
+    found.append([made, take()])
+    assert lib.tn_adamw_destroy(h) == 0
+print("RESULT " + json.dumps(found))
+"""
+
+
+def test_reset_master_is_one_launch_where_a_parameter_is_in_bf16():
+    import json
+    import subprocess
+    import sys
+    import tempfile
+    with tempfile.TemporaryDirectory() as folder:
+        out = os.path.join(folder, "libfake_hip.so")
+        subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I/opt/rocm/include", os.path.join(HERE, "fake_hip.cpp"), "-o", out])
+        env = dict(os.environ, LD_PRELOAD=out, PYTHONPATH=os.pathsep.join([HERE, os.path.dirname(HERE)]))
+        r = subprocess.run([sys.executable, "-c", RESET], cwd=os.path.dirname(HERE), env=env, capture_output=True, text=True, timeout=300)
+    lines = [l for l in r.stdout.splitlines() if l.startswith("RESULT ")]
+    assert lines, r.stderr[-800:]
+    (mixed_made, mixed), (_, f32), (_, empty) = json.loads(lines[0][7:])
+    assert mixed_made == [] and len(mixed) == 1 and "adamw_master_kernel" in mixed[0] and f32 == [] and empty == []

@@ -322,3 +322,42 @@ def test_refusals():
     opt.close()
     with pytest.raises(RuntimeError):
         opt.step([g, h])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_masters_set_anew_under_a_captured_step(bits):
+    """A step captured before reset_master() goes on from the new masters, as an eager one does; so does a captured reset_master()."""
+    a, b = (Setup(SIZES, "mixed", "f32", bits, seed=6) for _ in range(2))
+    step, reset = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    for s in (a, b):
+        s.opt.step(s.grads, max_norm=1.0)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(step):
+        norm = a.opt.step(a.grads, max_norm=1.0)
+    with torch.cuda.graph(reset):
+        a.opt.reset_master()
+    raw = lambda t: t.view(torch.uint8) if t.dim() else t      # noqa: E731
+    for i in range(4):
+        for s in (a, b):
+            for p, _ in s.params:
+                p.mul_(0.5 + i).add_(0.01)
+        a.opt.reset_master() if i < 2 else reset.replay()
+        b.opt.reset_master()
+        filler = [torch.full((n,), 7.0, device="cuda") for n in (1, 64, 4096, 65536)]          # what was freed would be taken
+        assert torch.equal(a.opt.state_dict()["master"], b.opt.state_dict()["master"])
+        step.replay()
+        want = b.opt.step(b.grads, max_norm=1.0)
+        torch.cuda.synchronize()
+        assert torch.equal(norm, want) and all(bool((f == 7.0).all()) for f in filler)
+        for k, v in a.opt.state_dict().items():
+            assert torch.equal(raw(v), raw(b.opt.state_dict()[k])), k
+        assert all(torch.equal(p, q) for (p, _), (q, _) in zip(a.params, b.params))
+        a.check_around()
+
+
+def test_reset_master_of_parameters_in_fp32_alone():
+    s = Setup([100, 50], "f32", "f32", 32)
+    s.opt.step(s.grads)
+    before = [p.clone() for p, _ in s.params]
+    s.opt.reset_master()
+    assert all(torch.equal(p, q) for (p, _), q in zip(s.params, before)) and int(s.opt.state_dict()["count"]) == 1
