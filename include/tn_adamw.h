@@ -9,7 +9,8 @@
  *     g <- g * max_norm / n             where there is a max_norm and n > max_norm
  *     m <- beta1 * m + (1 - beta1) * g,  v <- beta2 * v + (1 - beta2) * g^2
  *     p <- p * (1 - lr * decay) - lr * (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * all in fp32 (the powers, and what is made of them once a step, and n in 64 bits). With a max_norm and an n that is not finite nothing changes, the count
+ * all in fp32 (the powers, and what is made of them once a step, and n in 64 bits). lr * decay * p and the move are added up and taken off p in one subtraction, whose rounding, 2^-24 of p, is
+ * the only one at p's size: a decay below that is right on average over moves of different sizes (with no move beside it, it is lost). With a max_norm and an n that is not finite nothing changes, the count
  * neither. A parameter in bf16 is the rounding of an fp32 master, which is what the step reads and writes: a step of 1e-4 of a parameter's size would be
  * lost in its 8 bits.
  *

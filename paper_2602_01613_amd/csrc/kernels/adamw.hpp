@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(AdamwArgs a, Gradients 
     if (s.skip) return;
     const void* gp = grads.at(e.tensor);
     const bool g16 = grads.is_bf16(e.tensor);
-    const float keep = fmaf(-s.lr, t.decay, 1.f);
+    const float decay = s.lr * t.decay;
 #pragma unroll
     for (int i = 0; i < kPartValues / (256 * kChunk); ++i) {
         const int64_t at = int64_t(e.part) * kPartValues + (i * 256 + int(threadIdx.x)) * kChunk;
@@ -242,7 +242,10 @@ __global__ void __launch_bounds__(256) adamw_step_kernel(AdamwArgs a, Gradients 
             // (Cauchy and Schwarz over their past), and a smaller root is a rounding. (A comparison: a NaN stays one.)
             float under = root[q];
             if constexpr (BITS == 8) under = under < a.least * fabsf(m[q]) ? a.least * fabsf(m[q]) : under;
-            p[q] = fmaf(p[q], keep, -s.step * m[q] / fmaf(under, s.root_bias2, a.eps));
+            // Decay and move are taken off together. (As a factor 1 - decay the decay would be a multiple of 2^-24 of the parameter: 1.19 times itself at 1e-7, nothing at
+            // 1e-8. What is infinite stays so, as by the factor.)
+            const float move = s.step * m[q] / fmaf(under, s.root_bias2, a.eps);
+            p[q] -= fabsf(p[q]) < __builtin_inff() ? fmaf(decay, p[q], move) : move;
         }
         if (n) {
             if (t.bf16) {

@@ -361,3 +361,35 @@ def test_reset_master_of_parameters_in_fp32_alone():
     before = [p.clone() for p, _ in s.params]
     s.opt.reset_master()
     assert all(torch.equal(p, q) for (p, _), q in zip(s.params, before)) and int(s.opt.state_dict()["count"]) == 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr", [1e-5, 5e-6, 1e-6])
+def test_decay_far_below_a_parameters_last_place_is_right_on_average(bits, lr):
+    """lr * decay of 1e-8 to 1e-7, a sixth of fp32's half unit to more than one of it, taken off together with a move of another size for each value: the master's rounding is
+    off by at most 2^-24 of it, to either side, so that the mean over n values has a standard deviation of at most 2^-24 / sqrt(3 n). What the move adds is off by 2^-18 of it at most,
+    to either side too. A twentieth of the smallest decay, 5e-10, is more than seven of those, 6.7e-11 each."""
+    n, decay = 1 << 18, 0.01
+    rng = np.random.default_rng(11)
+    s = Setup([n], "f32", "f32", bits, weight_decay=decay)
+    s.params[0][0].copy_(torch.from_numpy(rng.uniform(0.02, 0.08, n) * rng.choice([-1, 1], n)))
+    for _ in range(5):
+        s.new_gradients()
+        s.opt.step(s.grads, lr=0.0)
+    before, states = s.values(), s.states()
+    s.new_gradients()
+    s.opt.step(s.grads, lr=lr)
+    exact, _, _ = O.step(before, s.flat(s.grads), *states, 6, lr, *BETAS, EPS, decay, 1.0, O.least_root(*BETAS) if bits == 8 else 0.0)
+    assert 7 * 2.0 ** -24 / (3 * n) ** 0.5 < 0.05 * lr * decay
+    off = ((s.values() - exact)[:n] / before[:n]).mean()
+    assert abs(off) < 0.05 * lr * decay, off / (lr * decay)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_parameter_that_is_infinite_stays_so(bits):
+    p = torch.full((300,), 0.5, device="cuda")
+    p[7], p[200] = float("inf"), float("-inf")
+    for decay in (0.0, 0.1):
+        opt = tn.AdamW([p], lr=LR, weight_decay=decay, state_bits=bits)
+        opt.step([torch.ones(300, device="cuda")])
+        assert float(p[7]) == float("inf") and float(p[200]) == float("-inf") and int(torch.isfinite(p).sum()) == 298
