@@ -13,6 +13,7 @@ import math
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .binding import TN_DTYPE_BF16, TN_DTYPE_F32, load_library
 from .fp8 import _CODES, _DTYPE, _SCALES, _check, _here, _stream
@@ -198,7 +199,8 @@ class AdamW:
         """One step with one gradient for each parameter (float32 or bfloat16, of its shape). lr: a number instead of the optimizer's, or a
         float32 tensor of one value, which a captured step reads at every replay. max_norm: gradients are scaled down to that norm over
         all of them; norm: that norm where it is known already (gradient_norm's, or one over several ranks). Returns the norm, None without
-        max_norm. Where it is not finite nothing changes."""
+        max_norm. Where it is not finite nothing changes. Parameters count as modified in place for autograd, as by torch's own optimizers (a replayed
+        step cannot say so)."""
         pointers, codes = self._gradients(grads)
         if [p.data_ptr() for p in self.params] != self._param_pointers:
             raise RuntimeError("a parameter's memory is not where it was when the optimizer was made")
@@ -222,6 +224,7 @@ class AdamW:
                 norm, space = torch.empty((), dtype=torch.float32, device=self._device), self._space()
         _check(_lib.tn_adamw_step(self._handle, pointers, codes, rate, rate_ptr, max_norm or 0.0, None if norm is None else norm.data_ptr(), int(given),
                                   None if space is None else space.data_ptr(), self._workspace_bytes, _stream(self._gpu)), "tn_adamw_step")
+        increment_version(self.params)
         return norm
 
     def state_dict(self) -> Dict[str, torch.Tensor]:

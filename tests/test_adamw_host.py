@@ -240,3 +240,18 @@ def test_reset_master_is_one_launch_where_a_parameter_is_in_bf16():
     assert lines, r.stderr[-800:]
     (mixed_made, mixed), (_, f32), (_, empty) = json.loads(lines[0][7:])
     assert mixed_made == [] and len(mixed) == 1 and "adamw_master_kernel" in mixed[0] and f32 == [] and empty == []
+
+
+def test_a_step_raises_the_parameters_versions(monkeypatch):
+    """What autograd saved before a step is not taken for the same after it; a step that was refused changes nothing."""
+    from fp8_util import on_gpu
+    params = [on_gpu(torch.zeros(5), 0), on_gpu(torch.zeros(3, dtype=torch.bfloat16), 0)]
+    opt, calls = _optimizer(monkeypatch, params)
+    before = [p._version for p in params]
+    grads = [on_gpu(torch.zeros(5), 0), on_gpu(torch.zeros(3), 0)]
+    with pytest.raises(ValueError):
+        opt.step(grads, lr=-1.0)
+    assert [p._version for p in params] == before and not calls
+    opt.step(grads)
+    assert [c[0] for c in calls] == ["tn_adamw_step"]
+    assert [p._version for p in params] == [v + 1 for v in before] and [g._version for g in grads] == [0, 0]

@@ -393,3 +393,16 @@ def test_a_parameter_that_is_infinite_stays_so(bits):
         opt = tn.AdamW([p], lr=LR, weight_decay=decay, state_bits=bits)
         opt.step([torch.ones(300, device="cuda")])
         assert float(p[7]) == float("inf") and float(p[200]) == float("-inf") and int(torch.isfinite(p).sum()) == 298
+
+
+def test_a_step_shows_in_the_parameters_version():
+    """What autograd saved before a step is refused after it, as with torch's own optimizers."""
+    p, q = torch.ones(100, device="cuda", requires_grad=True), torch.ones(50, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    opt = tn.AdamW([p, q])
+    grads = [torch.ones(100, device="cuda"), torch.ones(50, device="cuda")]
+    for t in (p, q):
+        loss = (t * t).sum()
+        opt.step(grads)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    (p * p).sum().backward()
