@@ -183,10 +183,13 @@ class AdamW:
     def gradient_norm(self, grads: Sequence[torch.Tensor], out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """sqrt(sum of the squares of all gradients) as a float32 tensor of one value, summed in 64 bits."""
         pointers, codes = self._gradients(grads)
-        out = torch.empty((), dtype=torch.float32, device=self._device) if out is None else self._scalar("out", out)
+        given = out is not None
+        out = self._scalar("out", out) if given else torch.empty((), dtype=torch.float32, device=self._device)
         space = self._space()
         _check(_lib.tn_adamw_gradient_norm(self._handle, pointers, codes, out.data_ptr(), space.data_ptr(), self._workspace_bytes, _stream(self._gpu)),
                "tn_adamw_gradient_norm")
+        if given:
+            increment_version(out)
         return out
 
     def _scalar(self, name: str, t: torch.Tensor) -> torch.Tensor:

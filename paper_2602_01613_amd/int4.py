@@ -13,6 +13,7 @@ import ctypes
 from typing import Optional, Sequence, Tuple
 
 import torch
+from torch.autograd.graph import increment_version
 
 from .binding import TN_DTYPE_BF16, TN_FLAG_TRANSPOSE, TN_QUERY_IN_FEATURES, TN_QUERY_OUT_FEATURES, load_library
 from .fp8 import _DTYPE, _check, _here, _matrix, _stream
@@ -131,7 +132,8 @@ class Int4Linear:
         if tokens > self.max_tokens:
             raise ValueError(f"x has {tokens} tokens: the layer was made for {self.max_tokens}")
         x_stride = _matrix("x", x, tokens, self.N, torch.bfloat16, gpu)
-        if out is None:
+        given = out is not None
+        if not given:
             out, stride = torch.empty((tokens, cols), dtype=torch.bfloat16, device=self._device), cols
         else:
             stride = _matrix("out", out, tokens, cols, torch.bfloat16, gpu)
@@ -141,6 +143,8 @@ class Int4Linear:
             _check(int(need), "tn_int4_linear_workspace")
         space = torch.empty((need,), dtype=torch.uint8, device=self._device) if need else None
         _check(fn(self._handle, x_ptr, x_stride, out.data_ptr(), stride, tokens, None if space is None else space.data_ptr(), need, _stream(gpu)), where)
+        if given:
+            increment_version(out)
         return out
 
     def forward(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -255,3 +255,11 @@ def test_a_step_raises_the_parameters_versions(monkeypatch):
     opt.step(grads)
     assert [c[0] for c in calls] == ["tn_adamw_step"]
     assert [p._version for p in params] == [v + 1 for v in before] and [g._version for g in grads] == [0, 0]
+
+
+def test_a_given_norm_tensor_counts_as_written(monkeypatch):
+    from fp8_util import on_gpu
+    opt, calls = _optimizer(monkeypatch, [on_gpu(torch.zeros(5), 0)])
+    out = on_gpu(torch.zeros(()), 0)
+    assert opt.gradient_norm([on_gpu(torch.zeros(5), 0)], out=out) is out
+    assert [c[0] for c in calls] == ["tn_adamw_gradient_norm"] and out._version == 1

@@ -157,3 +157,25 @@ def test_every_form_of_a_product_is_among_the_tested_sizes():
     want = {(k, t, s) for k in ("plain", "gated", "back") for t in TILES for s in (False, True)}
     want |= {("plain", 16, 1), ("plain", 16, 2), ("plain", 16, 4), ("plain", 32, 4), ("gated", 16, 2), ("gated", 16, 4), ("gated", 32, 4)}
     assert not want - seen, want - seen
+
+
+def test_a_given_output_counts_as_written(monkeypatch):
+    """For autograd, which may have saved it."""
+    from fp8_util import on_gpu
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: 0
+    monkeypatch.setattr(fp8, "_current_gpu", lambda: 0)
+    for name, value in (("_lib", Library()), ("_library", Library), ("_stream", lambda gpu: 99)):
+        monkeypatch.setattr(int4, name, value)
+    layer = tn.Int4Linear.__new__(tn.Int4Linear)
+    for name, value in dict(_handle=123, _gpu=0, _device="cpu", max_tokens=8, n_tensors=2, transpose=False, shape=(6, 10), M=12, N=10).items():
+        setattr(layer, name, value)
+    x, y, h = (on_gpu(torch.zeros(shape, dtype=torch.bfloat16), 0) for shape in ((3, 10), (3, 12), (3, 6)))
+    assert layer(x, out=y) is y and layer.gated(x, out=h) is h
+    assert (x._version, y._version, h._version) == (0, 1, 1)
+    with pytest.raises(ValueError):
+        layer(x, out=h)
+    assert h._version == 1
+    assert layer(x)._version == 0 and layer.gated(x)._version == 0
