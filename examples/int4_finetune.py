@@ -35,7 +35,7 @@ class Block:
     def _transposed(layer):
         """The gradients' layer with the same codes: groups lie along the inputs in both."""
         codes, scales, zeros = zip(*(layer.quantized_tensor(i) for i in range(layer.n_tensors)))
-        return tn.Int4Linear(codes, layer.max_tokens, transpose=True, group=layer.group, scales=[s.bfloat16() for s in scales], zeros=zeros,
+        return tn.Int4Linear(codes, layer.max_tokens, transpose=True, group=layer.group, scales=[s.to(layer.scale_dtype) for s in scales], zeros=zeros,
                              in_features=layer.shape[1])
 
     def _make_adapter(self):

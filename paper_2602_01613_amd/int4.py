@@ -119,6 +119,7 @@ class Int4Linear:
         del keep
         self._handle = int(h.value)
         self.shape, self.n_tensors, self.transpose, self.group = (desc.out_features, desc.in_features), desc.n_tensors, bool(transpose), desc.group
+        self.scale_dtype = torch.float16 if desc.scale_dtype == TN_DTYPE_F16 else torch.bfloat16
         self.max_tokens, self._device, self._gpu = int(max_tokens), first.device, gpu
         self.M, self.N = self.query(TN_QUERY_OUT_FEATURES), self.query(TN_QUERY_IN_FEATURES)
 
@@ -160,7 +161,8 @@ class Int4Linear:
         return self._run(_library().tn_int4_linear_gated, True, self.shape[0], x, out, "tn_int4_linear_gated")
 
     def quantized_tensor(self, slot: int = 0) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-        """(codes uint8 [M, ceil(N / 2)], scales float32 [M, ceil(N / group)], zeros uint8 likewise) of tensor `slot`."""
+        """(codes uint8 [M, ceil(N / 2)], scales float32 [M, ceil(N / group)], zeros uint8 likewise) of tensor `slot`. Another layer is made of
+        them with scales.to(layer.scale_dtype), the type they came in (bfloat16 where they were made here), which holds them exactly."""
         if self._handle is None:
             raise RuntimeError("layer was closed")
         gpu = _here("the layer", self._gpu)

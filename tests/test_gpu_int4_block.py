@@ -21,3 +21,20 @@ def test_block_and_its_step():
         errors = module.check(hidden, width, tokens, group)
         assert errors.pop("move") <= 1e-3, errors
         assert all(e < 16 * 2.0 ** -8 / 3 ** 0.5 for e in errors.values()), errors
+
+
+def test_the_way_back_has_the_weights_of_the_way_there():
+    """A checkpoint's fp16 scales have more bits than bf16 holds."""
+    import torch
+
+    import paper_2602_01613_amd as tn
+    spec = importlib.util.spec_from_file_location("int4_finetune", PATH)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    gen = torch.Generator().manual_seed(5)
+    codes = torch.randint(0, 256, (48, 150), generator=gen, dtype=torch.uint8).cuda()
+    scales = torch.rand((48, 10), generator=gen).half().cuda()
+    layer = tn.Int4Linear([codes], 4, group=32, scales=[scales])
+    back = module.Block._transposed(layer)
+    assert all(torch.equal(a, b) for a, b in zip(back.quantized_tensor(), layer.quantized_tensor()))
+    assert torch.equal(back.quantized_tensor()[1], scales.float())

@@ -335,3 +335,14 @@ def test_refusals():
     layer.close()
     with pytest.raises(RuntimeError):
         layer(x)
+
+
+@pytest.mark.parametrize("scale", ["bf16", "f16"])
+def test_a_layer_made_of_anothers_tensors_holds_the_same(scale):
+    """Scales come back in fp32, and scale_dtype is the type that holds them exactly."""
+    layer = layer_of(make(90, 300, 32, 1, True, scale), 300, 32, 1)
+    assert layer.scale_dtype == SCALE[scale]
+    codes, scales, zeros = layer.quantized_tensor()
+    again = tn.Int4Linear([codes], 1, transpose=True, group=32, scales=[scales.to(layer.scale_dtype)], zeros=[zeros], in_features=300)
+    assert all(torch.equal(a, b) for a, b in zip(again.quantized_tensor(), (codes, scales, zeros)))
+    assert tn.Int4Linear([torch.ones((4, 64), device="cuda")], 1).scale_dtype == torch.bfloat16
