@@ -77,7 +77,8 @@ int64_t tn_int4_linear_workspace(tn_int4_linear_t h, const void* x, int64_t x_st
 
 /*
  * y = X W^T in bf16, summed in fp32: x bf16 [tokens, N], y bf16 [tokens, n_tensors * M], the tensors' outputs beside each other. With TN_FLAG_TRANSPOSE: x
- * is [tokens, n_tensors * M], y is [tokens, N], the sum over the tensors of X_i W_i. y may not overlap x (TN_ERR_INVALID_ARG).
+ * is [tokens, n_tensors * M], y is [tokens, N], the sum over the tensors of X_i W_i. y may not overlap x (TN_ERR_INVALID_ARG): no
+ * element is of both; columns of the same rows, with one stride, lie beside each other. Of two different strides all between the first element and the last counts.
  * workspace: what the function above says, 256-byte aligned, for this call alone until its work is done: calls with workspaces of their own may be in
  * flight together. Nothing in it has to start at zero.
  * Rounding. Up to 64 tokens (where tn_int4_linear_plan_query says that the weight is streamed) products are taken with the codes as they are, which is exact,

@@ -22,9 +22,14 @@ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool aligned(const void* p, unsigned n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 int launched() { return hipGetLastError() == hipSuccess ? TN_OK : TN_ERR_HIP; }
 int64_t whole(int64_t bytes) { return div_up(bytes, 256) * 256; }
-bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
-    return p < q + uintptr_t(b_bytes) && q < p + uintptr_t(a_bytes);
+// Whether some element of x [rows, x_cols] is one of y [rows, y_cols], both of 2 bytes. Columns of the same rows may lie beside each other: with y's first element at
+// column d of x's rows, they are apart if d is past x's columns and y's end before the next row of x.
+bool overlap(const void* x, int64_t x_stride, int64_t x_cols, const void* y, int64_t y_stride, int64_t y_cols, int64_t rows) {
+    const intptr_t p = reinterpret_cast<intptr_t>(x), q = reinterpret_cast<intptr_t>(y);
+    if (p >= q + ((rows - 1) * y_stride + y_cols) * 2 || q >= p + ((rows - 1) * x_stride + x_cols) * 2) return false;
+    if (x_stride != y_stride || rows == 1) return true;
+    const int64_t row = x_stride * 2, d = ((q - p) % row + row) % row;
+    return d < x_cols * 2 || d + y_cols * 2 > row;
 }
 
 }  // namespace
@@ -316,7 +321,7 @@ int run_product(const tn_int4_linear_s& h, const void* x, int64_t x_stride, void
     const int64_t x_cols = h.k_segments * h.k_cols, y_cols = gated ? h.features : int64_t(h.out_segments) * h.features;
     if (!x || !y || x_stride < x_cols || y_stride < y_cols || !aligned(x, 2) || !aligned(y, 2)) return TN_ERR_INVALID_ARG;
     // workgroups read rows of x while others write theirs of y
-    if (overlap(x, ((tokens - 1) * x_stride + x_cols) * 2, y, ((tokens - 1) * y_stride + y_cols) * 2)) return TN_ERR_INVALID_ARG;
+    if (overlap(x, x_stride, x_cols, y, y_stride, y_cols, tokens)) return TN_ERR_INVALID_ARG;
     Int4Args a = product_args(h, x, x_stride, tokens);
     const Choice c = choose(a, gated);
     const Workspace w = workspace_of(h, a, c);

@@ -149,7 +149,8 @@ class Int4Linear:
         return out
 
     def forward(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """bf16 [tokens, M] for bf16 x [tokens, N] (rows may have a stride); two tensors' outputs lie beside each other. out may not overlap x."""
+        """bf16 [tokens, M] for bf16 x [tokens, N] (rows may have a stride); two tensors' outputs lie beside each other. out may not overlap x:
+        columns of one buffer beside each other are apart."""
         return self._run(_library().tn_int4_linear_forward, False, self.M, x, out, "tn_int4_linear_forward")
 
     __call__ = forward

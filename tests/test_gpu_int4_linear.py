@@ -346,3 +346,18 @@ def test_a_layer_made_of_anothers_tensors_holds_the_same(scale):
     again = tn.Int4Linear([codes], 1, transpose=True, group=32, scales=[scales.to(layer.scale_dtype)], zeros=[zeros], in_features=300)
     assert all(torch.equal(a, b) for a, b in zip(again.quantized_tensor(), (codes, scales, zeros)))
     assert tn.Int4Linear([torch.ones((4, 64), device="cuda")], 1).scale_dtype == torch.bfloat16
+
+
+@pytest.mark.parametrize("tokens", [1, 20, 64, 65, 200])
+def test_input_and_output_beside_each_other_in_one_buffer(tokens):
+    """Columns of the same rows share no element: outputs go beside the inputs, to either side, and nothing else is written."""
+    m, n = 130, 384
+    layer, x = layer_of(make(m, n, 64, 1), n, 64, tokens), rows(tokens, n).cuda()
+    want = layer(x)
+    for x_at, y_at in ((0, n), (m, 0), (m + 5, 3)):
+        wide = torch.full((tokens, m + n + 9), 7.0, dtype=torch.bfloat16, device="cuda")
+        wide[:, x_at:x_at + n] = x
+        expect = wide.clone()
+        expect[:, y_at:y_at + m] = want
+        layer(wide[:, x_at:x_at + n], out=wide[:, y_at:y_at + m])
+        assert torch.equal(wide, expect)

@@ -179,3 +179,47 @@ def test_a_given_output_counts_as_written(monkeypatch):
         layer(x, out=h)
     assert h._version == 1
     assert layer(x)._version == 0 and layer.gated(x)._version == 0
+
+
+BESIDE = """
+import ctypes, json
+import paper_2602_01613_amd as tn
+from paper_2602_01613_amd import int4
+import test_int4_host as host
+lib = int4._library()
+mem = ctypes.create_string_buffer(1 << 20)
+at = (ctypes.addressof(mem) + 255) // 256 * 256
+space = at + (1 << 19)
+desc, keep = host._desc(out_features=20, in_features=32, tensors=[at], scales=[at])
+h = ctypes.c_void_p(0)
+assert lib.tn_int4_linear_create(ctypes.byref(h), ctypes.byref(desc)) == 0
+def status(x_at, x_stride, y_at, y_stride, tokens):
+    base = at + 4096
+    return lib.tn_int4_linear_forward(h, base + 2 * x_at, x_stride, base + 2 * y_at, y_stride, tokens, space, 1 << 18, None)
+print("RESULT " + json.dumps([status(*case) for case in json.loads(CASES)]))
+"""
+
+
+def test_input_and_output_may_lie_beside_each_other():
+    """Against the sets of their elements, where the strides are equal; of different strides, against the spans."""
+    import json
+    import subprocess
+    import sys
+    import tempfile
+    cases = [(x, s, y, s, t) for s in (32, 40, 52, 55, 60, 104) for t in (1, 2, 5) for x, y in
+             [(0, d) for d in (0, 19, 20, 31, 32, 35, 40, 51, 52, 60, 84, 104, 136, 300)] + [(d, 0) for d in (1, 19, 20, 23, 25, 28, 32, 40, 52, 72, 75, 124, 300)]]
+    cases += [(0, 64, 32, 65, 3), (0, 64, 160, 65, 3), (0, 64, 159, 65, 3), (200, 64, 0, 90, 3), (199, 64, 0, 90, 3)]
+    with tempfile.TemporaryDirectory() as folder:
+        out = os.path.join(folder, "libfake_hip.so")
+        subprocess.check_call(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I/opt/rocm/include", os.path.join(HERE, "fake_hip.cpp"), "-o", out])
+        env = dict(os.environ, LD_PRELOAD=out, PYTHONPATH=os.pathsep.join([HERE, os.path.dirname(HERE)]))
+        r = subprocess.run([sys.executable, "-c", f"CASES = {json.dumps(json.dumps(cases))}\n" + BESIDE], cwd=os.path.dirname(HERE), env=env, capture_output=True, text=True, timeout=300)
+    lines = [l for l in r.stdout.splitlines() if l.startswith("RESULT ")]
+    assert lines, r.stderr[-800:]
+    for (x, sx, y, sy, t), status in zip(cases, json.loads(lines[0][7:])):
+        if sx == sy:
+            mine, other = ({at + i * sx + c for i in range(t) for c in range(cols)} for at, cols in ((x, 32), (y, 20)))
+            apart = not mine & other
+        else:
+            apart = x >= y + (t - 1) * sy + 20 or y >= x + (t - 1) * sx + 32
+        assert status == (0 if apart else INVALID), (x, sx, y, sy, t, status)
