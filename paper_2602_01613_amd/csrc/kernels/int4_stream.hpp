@@ -84,12 +84,14 @@ struct StreamBlock {
     unsigned words[GROUPS][SUB];
     bf16x8 x[TG][4];
 };
-template <int TG>
-constexpr int kRing = TG == 2 ? 3 : 4;
+// Blocks in flight, as many as registers hold: of 32 tokens three, and two where a block has four groups' words (three kept 40 registers in scratch memory: 24 tokens, 5120 -> 25600 in groups
+// of 32, 52 us, 30 with two; with groups of 128, 28).
+template <int TG, int SUB>
+constexpr int kRing = TG == 1 ? 4 : SUB == 4 ? 2 : 3;
 
 template <int GROUPS, int TG, int SUB, bool GATED>
 __global__ void __launch_bounds__(512) int4_stream_kernel(Int4Args a) {
-    constexpr int RING = kRing<TG>;
+    constexpr int RING = kRing<TG, SUB>;
     __shared__ floatx4 part[8][GROUPS][TG][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     // gated: the first half of the pieces are gate's, the others up's

@@ -223,3 +223,40 @@ def test_input_and_output_may_lie_beside_each_other():
         else:
             apart = x >= y + (t - 1) * sy + 20 or y >= x + (t - 1) * sx + 32
         assert status == (0 if apart else INVALID), (x, sx, y, sy, t, status)
+
+
+def _kernels(path):
+    """(name, notes) of the gfx950 kernels in a library that was built here: the metadata of its code objects."""
+    import struct
+
+    import msgpack
+    data = open(path, "rb").read()
+    at = data.find(b"__CLANG_OFFLOAD_BUNDLE__")
+    while at >= 0:
+        n, p = struct.unpack_from("<Q", data, at + 24)[0], at + 32
+        for _ in range(n):
+            start, size, length = struct.unpack_from("<QQQ", data, p)
+            target, p = data[p + 24:p + 24 + length], p + 24 + length
+            if b"gfx950" not in target or not size:
+                continue
+            elf = data[at + start:at + start + size]
+            headers, (step, count) = struct.unpack_from("<Q", elf, 32)[0], struct.unpack_from("<HH", elf, 54)
+            for i in range(count):
+                kind, _, where, _, _, held = struct.unpack_from("<IIQQQQ", elf, headers + i * step)
+                end = where + held if kind == 4 else 0                    # 4: notes
+                while where < end:
+                    name, size_of, what = struct.unpack_from("<III", elf, where)
+                    body = where + 12 + (name + 3) // 4 * 4
+                    if what == 32:                                        # AMDGPU metadata
+                        for kernel in msgpack.unpackb(elf[body:body + size_of])["amdhsa.kernels"]:
+                            yield kernel[".name"], kernel
+                    where = body + (size_of + 3) // 4 * 4
+        at = data.find(b"__CLANG_OFFLOAD_BUNDLE__", at + 24)
+
+
+def test_no_kernel_keeps_registers_in_memory():
+    """A register that does not fit goes to scratch memory, and comes back from it in the inner loop."""
+    found = {name: k for name, k in _kernels(tn.library_path()) if re.search(r"int4_|adamw_|gradient_norm", name)}
+    assert sum("int4_stream_kernel" in n for n in found) == 21 and sum("int4_gemm_kernel" in n for n in found) == 78 and len(found) > 105
+    spilled = [n for n, k in found.items() if k[".vgpr_spill_count"] or k[".sgpr_spill_count"] or k[".private_segment_fixed_size"]]
+    assert not spilled, spilled
