@@ -7,7 +7,7 @@ import torch
 import oracle.int4_oracle as I
 import paper_2602_01613_amd as tn
 from fp8_util import half_unit, host
-from int4_util import FORM_CASES
+from int4_util import FORM_CASES, GROUP_CASES
 
 pytestmark = pytest.mark.gpu
 
@@ -361,3 +361,30 @@ def test_input_and_output_beside_each_other_in_one_buffer(tokens):
         expect[:, y_at:y_at + m] = want
         layer(wide[:, x_at:x_at + n], out=wide[:, y_at:y_at + m])
         assert torch.equal(wide, expect)
+
+
+def dense(x, w):
+    """x @ w in 64 bits: on the GPU, where hundreds of such products take no time."""
+    return host(torch.matmul(x.cuda().double(), torch.from_numpy(np.ascontiguousarray(w)).cuda()))
+
+
+@pytest.mark.parametrize("kind,tokens,m,n,group", [(*c[:4], g) for c in GROUP_CASES for g in c[4]])
+def test_every_kernel(kind, tokens, m, n, group):
+    made = make(m, n, group, 2 if kind == "gated" else 1, group != 64, "f16" if tokens % 2 else "bf16", seed=tokens + m + group)
+    w = weights_of(made, group)
+    if kind == "back":
+        layer, dy = layer_of(made, n, group, tokens, transpose=True), rows(tokens, m, 4, 1e-3)
+        check(layer(dy.cuda()), dense(dy, w[0]), (2.0 ** -11 + (m + 16) * 2.0 ** -23) * dense(dy.abs(), np.abs(w[0])))
+        return
+    layer, x = layer_of(made, n, group, tokens), rows(tokens, n)
+    exact_codes = streamed(m, n, len(made), tokens, kind == "gated", group)
+    off = []
+    for (c, s, z), v in zip(made, w):          # as in bounds()
+        terms = (c + 32.0 + (8 if z is None else np.repeat(z, group, axis=1)[:, :n])) * np.repeat(np.abs(s.double().numpy()), group, axis=1)[:, :n] if exact_codes else np.abs(v)
+        off.append(((group + 4 + n / group + 16) * 2.0 ** -23 if exact_codes else 2.0 ** -11 + (n + 16) * 2.0 ** -23) * dense(x.abs(), terms.T))
+    sums = [dense(x, v.T) for v in w]
+    if kind == "plain":
+        check(layer(x.cuda()), sums[0], off[0])
+    else:
+        ref = I.silu_gate(*sums)
+        check(layer.gated(x.cuda()), ref, 1.1 * off[0] * (np.abs(sums[1]) + off[1]) + np.abs(sums[0]) * off[1] + 2.0 ** -20 * (np.abs(ref) + 1e-30))

@@ -260,3 +260,20 @@ def test_no_kernel_keeps_registers_in_memory():
     assert sum("int4_stream_kernel" in n for n in found) == 21 and sum("int4_gemm_kernel" in n for n in found) == 78 and len(found) > 105
     spilled = [n for n, k in found.items() if k[".vgpr_spill_count"] or k[".sgpr_spill_count"] or k[".private_segment_fixed_size"]]
     assert not spilled, spilled
+
+
+def test_every_compiled_kernel_is_among_the_tested_sizes():
+    """Tiles by tokens, output, direction and groups to 128 inputs (transposed: groups of features to a wave's 64), streams by tokens, pieces, output and groups."""
+    from int4_util import GROUP_CASES
+    seen = set()
+    for kind, tokens, m, n, groups in GROUP_CASES:
+        for group in groups:
+            ask = lambda what: tn.int4_plan_query(m, n, 2 if kind == "gated" else 1, tokens, kind == "gated", what, kind == "back", group)      # noqa: E731
+            tile, ranges = ask(tn.TN_INT4_PLAN_TILE_TOKENS), ask(tn.TN_INT4_PLAN_RANGES)
+            sub = 128 // group if kind != "back" else 2 if group == 32 else 1
+            seen.add((kind, tile, ranges > 1, sub) if tile else (kind, ask(tn.TN_INT4_PLAN_STREAM_TOKENS), ask(tn.TN_INT4_PLAN_STREAM_PIECES), sub))
+            blocks = -(-(m if kind == "back" else n) // 128)
+            assert -(-blocks // ranges) >= 6, (kind, tokens, m, n, group)
+    want = {(k, t, s, u) for k in ("plain", "gated") for t in TILES for s in (False, True) for u in (1, 2, 4)} | {("back", t, s, u) for t in TILES for s in (False, True) for u in (1, 2)}
+    want |= {("plain", t, p, u) for t, p in ((16, 1), (16, 2), (16, 4), (32, 4)) for u in (1, 2, 4)} | {("gated", t, p, u) for t, p in ((16, 2), (16, 4), (32, 4)) for u in (1, 2, 4)}
+    assert not want - seen, want - seen
