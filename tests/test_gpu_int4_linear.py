@@ -7,7 +7,7 @@ import torch
 import oracle.int4_oracle as I
 import paper_2602_01613_amd as tn
 from fp8_util import half_unit, host
-from int4_util import FORM_CASES, GROUP_CASES
+from int4_util import FORM_CASES, GROUP_CASES, LONG_ROWS
 
 pytestmark = pytest.mark.gpu
 
@@ -388,3 +388,30 @@ def test_every_kernel(kind, tokens, m, n, group):
     else:
         ref = I.silu_gate(*sums)
         check(layer.gated(x.cuda()), ref, 1.1 * off[0] * (np.abs(sums[1]) + off[1]) + np.abs(sums[0]) * off[1] + 2.0 ** -20 * (np.abs(ref) + 1e-30))
+
+
+@pytest.mark.parametrize("tokens,m,n,tensors,transposed,ranges,runs", LONG_ROWS)
+def test_every_run_of_long_rows(tokens, m, n, tensors, transposed, ranges, runs):
+    """Rows of one value each, which together have one in every run of 8 inputs: an output is that value, from 2^-20 to 2^20, times a weight rounded to fp16, and each row's power of two hangs
+    on a run of its own. Then rows full of values: a run that was lost or taken twice among r of them is off by sqrt(1 / r) in the mean square, 1.2 % or more; the roundings
+    are 2^-8 / sqrt(3), and the weights' a tenth of that, as above."""
+    made = make(m, n, 128, tensors, True, "f16", seed=runs)
+    layer = layer_of(made, n, 128, tokens, transpose=transposed)
+    w = weights_of(made, 128)
+    w = np.concatenate(w) if transposed else w[0].T              # [inputs, outputs]
+    own = m if transposed else n                                 # inputs of a tensor: runs start anew with each, at a multiple of 128
+    per = -(-own // 128) * 16
+    rng = np.random.default_rng(8)
+    run = np.arange(tokens) % (tensors * per)
+    column = run // per * own + np.minimum(run % per * 8 + rng.integers(0, 8, tokens), own - 1)
+    assert len(np.unique(column)) >= tensors * -(-own // 8)
+    value = torch.from_numpy(rng.standard_normal(tokens) * np.exp2(rng.integers(-20, 21, tokens))).bfloat16()
+    x = torch.zeros((tokens, tensors * own), dtype=torch.bfloat16, device="cuda")
+    x[torch.arange(tokens), torch.from_numpy(column)] = value.cuda()
+    ref = host(value)[:, None] * w[column]
+    check(layer(x), ref, 2.0 ** -11 * np.abs(ref))
+    x = torch.randn((tokens, tensors * own), generator=torch.Generator(device="cuda").manual_seed(9), dtype=torch.bfloat16, device="cuda")
+    y = layer(x)
+    some = torch.arange(0, tokens, tokens // 61)
+    ref = dense(x[some], w)
+    assert np.linalg.norm(host(y[some]) - ref) <= 1.1 * 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(ref)

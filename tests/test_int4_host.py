@@ -277,3 +277,15 @@ def test_every_compiled_kernel_is_among_the_tested_sizes():
     want = {(k, t, s, u) for k in ("plain", "gated") for t in TILES for s in (False, True) for u in (1, 2, 4)} | {("back", t, s, u) for t in TILES for s in (False, True) for u in (1, 2)}
     want |= {("plain", t, p, u) for t, p in ((16, 1), (16, 2), (16, 4), (32, 4)) for u in (1, 2, 4)} | {("gated", t, p, u) for t, p in ((16, 2), (16, 4), (32, 4)) for u in (1, 2, 4)}
     assert not want - seen, want - seen
+
+
+def test_long_rows_are_as_long_as_they_are_meant_to_be():
+    from int4_util import LONG_ROWS
+    for tokens, m, n, tensors, transposed, ranges, runs in LONG_ROWS:
+        assert tn.int4_plan_query(m, n, tensors, tokens, False, tn.TN_INT4_PLAN_TILE_TOKENS, transposed) > 0
+        assert tn.int4_plan_query(m, n, tensors, tokens, False, tn.TN_INT4_PLAN_RANGES, transposed) == ranges
+        blocks = tensors * -(-m // 128) if transposed else -(-n // 128)
+        assert -(-blocks // ranges) * 16 == runs
+    runs = [r[-1] for r in LONG_ROWS]
+    assert any(512 < r <= 1024 for r in runs) and any(1024 < r <= 3328 for r in runs) and any(r > 3328 for r in runs)
+    assert any(t == 2 and back and -(-m // 128) * 16 > 3328 for _, m, _, t, back, _, _ in LONG_ROWS)          # the second tensor's part begins behind what threads hold
