@@ -83,7 +83,8 @@ int64_t tn_int4_linear_workspace(tn_int4_linear_t h, const void* x, int64_t x_st
  * flight together. Nothing in it has to start at zero.
  * Rounding. Up to 64 tokens (where tn_int4_linear_plan_query says that the weight is streamed) products are taken with the codes as they are, which is exact,
  * and fp32 sums of a group are multiplied with its scale. In tiles, weights are rounded to fp16 under a power of two for each feature (with TN_FLAG_TRANSPOSE for each
- * group of features): off by 2^-11 of themselves, or by 2^-35 of the largest scale of the feature (group) where that is more; and tokens are in fp16 under a power of two for
+ * group of features): off by 2^-11 of themselves, and where their scale is below 2^-24 of the largest scale of the feature (group) by up to 2^-31 of that largest on top (the scale is off by
+ * 2^-35 of it, the weight by up to 15 times that); and tokens are in fp16 under a power of two for
  * each row (each range of a row, where the inputs are split), which is exact, or off by 2^-39 of the row's largest finite magnitude. Sums are fp32's (in the matrix cores). Infinities and NaN of a token show in its row alone, and as
  * sums of W[f][k] * x[k] have them.
  */

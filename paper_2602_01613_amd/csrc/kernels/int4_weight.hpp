@@ -14,8 +14,8 @@
 // segment, with words of scale 0.
 //
 // Tiles multiply in fp16, for which there is a second word to a group: scale / 2^e in fp16 and -(1024 + zero), with e of the feature (transposed: of the group of
-// features) such that the largest of its scales is in [2^10, 2^11). A weight is at most 15 of them, and scales down to 2^-25 of the largest keep all
-// their bits. They lie like the others, but transposed the scales and the zeros of 8 k beside each other: [feature / group][k / 8][2][8] halves.
+// features) such that the largest of its scales is in [2^10, 2^11). A weight is at most 15 of them. Scales down to 2^-24 of the largest keep all
+// their bits; below, where fp16 is subnormal, they are off by 2^-35 of the largest at most, and the weight by 15 times that. They lie like the others, but transposed the scales and the zeros of 8 k beside each other: [feature / group][k / 8][2][8] halves.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPiece = 16, kPieceWords = 256, kFeaturePad = 64;
 

@@ -415,3 +415,25 @@ def test_every_run_of_long_rows(tokens, m, n, tensors, transposed, ranges, runs)
     some = torch.arange(0, tokens, tokens // 61)
     ref = dense(x[some], w)
     assert np.linalg.norm(host(y[some]) - ref) <= 1.1 * 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("scale", ["f16", "bf16"])
+@pytest.mark.parametrize("transpose", [False, True])
+def test_scales_of_one_feature_far_apart_in_tiles(transpose, scale):
+    """Scales from 1 to 2^-24 of the largest of a feature (transposed: of a group of features) in fp16, to 2^-30 in bf16, and tokens that read one of them alone: a weight is off by 2^-11 of itself and by
+    2^-31 of the largest scale. The sums of the token's 32 values add 2^-23 for each."""
+    m, n, group, tokens = 96, 512, 32, 192
+    codes, s, z = make(m, n, group, 1, seed=12)[0]
+    down = torch.arange(m)[:, None] / (m - 1) if transpose else torch.arange(n // group)[None, :] / (n // group - 1)
+    s = (torch.sign(s.float()) * (1 + torch.rand(s.shape, generator=torch.Generator().manual_seed(1))) * torch.exp2(-torch.round((24 if scale == "f16" else 30) * down))).to(SCALE[scale])
+    made = [(codes, s, z)]
+    layer, w = layer_of(made, n, group, tokens, transpose=transpose), weights_of(made, group)[0]
+    assert tn.int4_plan_query(m, n, 1, tokens, False, tn.TN_INT4_PLAN_TILE_TOKENS, transpose, group) > 0
+    x = rows(tokens, m if transpose else n).float()
+    own = (torch.arange(m)[None, :] if transpose else torch.arange(n)[None, :] // group) == torch.arange(tokens)[:, None] % (m if transpose else n // group)
+    x = (x * own).bfloat16()
+    size = np.abs(s.double().numpy())
+    most = np.repeat(size.max(axis=0), group) if transpose else size.max(axis=1)             # of each output
+    w = w if transpose else w.T
+    sums = np.abs(host(x)) @ np.abs(w)
+    check(layer(x.cuda()), host(x) @ w, (2.0 ** -11 + 48 * 2.0 ** -23) * sums + 2.0 ** -31 * np.abs(host(x)).sum(axis=1, keepdims=True) * most)

@@ -289,3 +289,19 @@ def test_long_rows_are_as_long_as_they_are_meant_to_be():
     runs = [r[-1] for r in LONG_ROWS]
     assert any(512 < r <= 1024 for r in runs) and any(1024 < r <= 3328 for r in runs) and any(r > 3328 for r in runs)
     assert any(t == 2 and back and -(-m // 128) * 16 > 3328 for _, m, _, t, back, _, _ in LONG_ROWS)          # the second tensor's part begins behind what threads hold
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+def test_bound_of_weights_in_tiles(kind):
+    """A scale as fp16 under the power of two that puts the largest into [2^10, 2^11), times a code, rounded again: off by 2^-11 of the weight and, of scales below 2^-24 of the largest, by
+    2^-31 of that largest. Half of the latter would not do."""
+    rng = np.random.default_rng(2)
+    bits = 11 if kind == "f16" else 8
+    largest = np.exp2(rng.uniform(0, 1, 1 << 18))
+    part, e = np.frexp(largest * np.exp2(-rng.uniform(0, 40, largest.size)))
+    scale = np.ldexp(np.round(part * 2 ** bits) / 2 ** bits, e)
+    half = (scale * 1024).astype(np.float16)
+    assert (half.astype(np.float64) / 1024 == scale)[scale >= 2.0 ** -24 * largest].all()
+    codes = np.arange(1, 16)[:, None]
+    off = np.abs((codes.astype(np.float16) * half).astype(np.float64) / 1024 - codes * scale) - 2.0 ** -11 * codes * scale
+    assert 2.0 ** -32 < (off / largest).max() <= 2.0 ** -31
