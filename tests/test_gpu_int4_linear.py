@@ -437,3 +437,15 @@ def test_scales_of_one_feature_far_apart_in_tiles(transpose, scale):
     w = w if transpose else w.T
     sums = np.abs(host(x)) @ np.abs(w)
     check(layer(x.cuda()), host(x) @ w, (2.0 ** -11 + 48 * 2.0 ** -23) * sums + 2.0 ** -31 * np.abs(host(x)).sum(axis=1, keepdims=True) * most)
+
+
+@pytest.mark.parametrize("transpose", [False, True])
+def test_more_tokens_than_one_launch_converts(transpose):
+    """Rows become fp16 2^19 at a time."""
+    m, n, tokens = 24, 40, (1 << 19) + 4099
+    made = make(m, n, 32, 2 if transpose else 1, seed=13)
+    layer = layer_of(made, n, 32, tokens, transpose=transpose)
+    w = weights_of(made, 32)
+    w = np.concatenate(w) if transpose else w[0].T
+    x = torch.randn((tokens, len(w)), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").bfloat16()
+    check(layer(x), dense(x, w), (2.0 ** -11 + (len(w) + 16) * 2.0 ** -23) * dense(x.abs(), np.abs(w)))
