@@ -27,7 +27,8 @@
  * rounded to 2^-20.) What is not finite becomes a NaN code and stays out of its block's scale.
  * Where beta1^2 < beta2, |m| <= B sqrt(v) with B = (1 - beta1) / sqrt((1 - beta2) (1 - beta1^2 / beta2)), 7.3 for 0.9 and 0.999, whatever the gradients were; a root that is
  * less than |m| / B is one that was rounded (to zero, beside values 2^18 times larger in its block), and in 8 bits the step divides by |m| / B in its place: without that one
- * such value moves by m / eps.
+ * such value moves by m / eps. That holds for states that began at zero with these betas. One loaded from a run with others, or made elsewhere, may have such roots without any
+ * rounding: the steps of those values are shorter than the formula's, until m has forgotten (states in 32 bits are taken as they are).
  */
 #ifndef TN_ADAMW_H
 #define TN_ADAMW_H

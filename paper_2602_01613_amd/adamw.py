@@ -91,7 +91,8 @@ class AdamW:
     of them, and lives on the GPU that is current when it is made and has to be current when it is used.
 
     weight_decay  one number, or one for each tensor (none for norms' weights, say)
-    state_bits    32: m and v in fp32; 8: m and sqrt(v) in e4m3 with a scale for each 128 and rounding at random, 2.02 bytes a value instead of 8
+    state_bits    32: m and v in fp32; 8: m and sqrt(v) in e4m3 with a scale for each 128 and rounding at random, 2.02 bytes a value instead of 8,
+                  and the step divides by no less than the least sqrt(v) that gradients can leave beside that m
     seed          of that rounding: whoever starts again from a state_dict() with the same seed gets the same results
 
     A bfloat16 parameter is the rounding of an fp32 master held here, so that whoever sets it from outside calls reset_master(). Steps
@@ -236,7 +237,8 @@ class AdamW:
         return dict(self._state)
 
     def load_state_dict(self, state: Dict[str, torch.Tensor]) -> None:
-        """Copies a state of the same parameters and state_bits; parameters are loaded by whoever owns them."""
+        """Copies a state of the same parameters and state_bits; parameters are loaded by whoever owns them. In 8 bits a root of v below what these
+        betas allow beside its m is taken for a rounding (include/tn_adamw.h), also where the state is one of other betas."""
         if set(state) != set(self._state):
             raise ValueError(f"a state of this optimizer has {sorted(self._state)}, not {sorted(state)}")
         for key, t in self._state.items():

@@ -406,3 +406,20 @@ def test_a_step_shows_in_the_parameters_version():
         with pytest.raises(RuntimeError, match="modified by an inplace operation"):
             loss.backward()
     (p * p).sum().backward()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_of_other_betas(bits):
+    """After one gradient m = (1 - beta1) g and v = (1 - beta2) g^2, so that betas of 0.5 and 0.999 leave m = 15.8 sqrt(v): more than 0.9 and 0.999 can, 7.3. States in 32 bits go on by the formula, in 8
+    bits the step divides by |m| / B, as documented; check_step knows of both."""
+    n = 1000
+    first = tn.AdamW([torch.zeros(n, device="cuda")], lr=0.0, betas=(0.5, 0.999), state_bits=bits)
+    s = Setup([n], "f32", "f32", bits, seed=21)
+    first.step(s.grads)
+    s.opt.load_state_dict(first.state_dict())
+    before, states = s.values(), s.states()
+    least = O.least_root(*BETAS)
+    assert (np.sqrt(states[1]) < least * np.abs(states[0]))[:n].mean() > 0.9
+    s.new_gradients(1e-4)
+    s.opt.step(s.grads)
+    check_step(s, before, states, 2, s.states())
