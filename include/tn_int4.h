@@ -112,7 +112,7 @@ int tn_int4_linear_tensor(tn_int4_linear_t h, int32_t slot, void* codes, void* s
 /* what: TN_QUERY_OUT_FEATURES and TN_QUERY_IN_FEATURES (columns of y and of x, all segments), TN_QUERY_PACKED_BYTES, TN_QUERY_PARAM_COUNT */
 int tn_int4_linear_query(tn_int4_linear_t h, int32_t what, int64_t* value);
 
-/* No call may be in flight. NULL is accepted. */
+/* No call may be in flight, and no graph that captured one may be replayed afterwards. NULL is accepted. */
 int tn_int4_linear_destroy(tn_int4_linear_t h);
 
 #ifdef __cplusplus

@@ -17,7 +17,7 @@
 //
 // Measured: 8192 x 5120 -> 25600 in 1745 us, 1.23 PFLOP/s (the vendor library's bf16 product of the same sizes 1775), matrix cores busy 56 % of the cycles at 2.1 GHz; 77 x
 // 51200 -> 5120 (transposed) 62 us, busy 32 %. What bounds it is the one wave of each SIMD: its conversions (60 instructions of four cycles a step) hide only in part behind 4 * TM MFMAs of 16, so that
-// a step takes about 140 ns more than its MFMAs at any TM, and large tiles are best wherever they fill the chip. More stages of tokens in LDS (four to six), and codes and
+// a step takes longer than its MFMAs, by 160 ns with 32 tokens, 180 with 96 and 230 with 192, and large tiles are best wherever they fill the chip. More stages of tokens in LDS (four to six), and codes and
 // scale words read a step ahead of their use, changed nothing (1 %).
 // ---------------------------------------------------------------------------------------------
 enum Int4Form : int { INT4_PLAIN = 0, INT4_GATED = 1, INT4_PARTIAL = 2 };

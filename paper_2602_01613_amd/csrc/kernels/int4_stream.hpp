@@ -50,7 +50,7 @@ __device__ __forceinline__ float plain_sum(const unsigned* packed, const unsigne
     return sum;
 }
 
-// silu(gate) * up: relative error 2^-20, finite for every finite gate
+// silu(gate) * up: relative error 2^-20 down to gates of -87, below which the sigmoid is under fp32's least normal and comes out as 0; finite for every finite gate
 __device__ __forceinline__ float gated_value(float gate, float up) { return gate * sigmoid(gate) * up; }
 
 __device__ __forceinline__ bool is_finite(float v) { return (__float_as_uint(v) & 0x7fffffffu) < 0x7f800000u; }

@@ -159,7 +159,7 @@ struct Choice {
 // all: with more tokens more pieces (25600 outputs of 5120 inputs, 16 tokens: 21 us with four, 31 with two, 46 with one), and 32 tokens at a time. Where there are few
 // outputs, a workgroup's own time counts, the blocks of k that its waves take one after another: one piece (1024 outputs, 64 tokens: 11 us, 20 with 64 tokens to a workgroup), and
 // eight waves instead of four (25600 -> 5120, one token: 19 us, 22 with four). Elsewhere four, so that a CU has several workgroups, one of them at its beginning or
-// end while others stream (gated 25600 outputs, one token: 35 us, 45 with eight).
+// end while others stream (gated 25600 outputs, one token: 34 us in a graph, 46 with eight).
 constexpr struct {
     int groups, tg;
 } kStreams[] = {{1, 1}, {2, 1}, {4, 1}, {4, 2}};

@@ -96,7 +96,7 @@ def int4_plan_query(out_features: int, in_features: int, n_tensors: int, tokens:
 
 class Int4Linear:
     """One 4-bit weight [M, N], or two that read the same activations (gate and up), living on the GPU that is current when it is made
-    and has to be current when it is used.
+    and has to be current when it is used. Graphs that captured its calls are not replayed after close().
 
     tensors  one or two contiguous CUDA tensors: [M, N] of float32 or bfloat16, quantised in groups along N; or, with `scales`, uint8 codes
              [M, ceil(N / 2)], two to a byte with the even input in the low half
