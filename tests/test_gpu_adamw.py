@@ -423,3 +423,30 @@ def test_a_state_of_other_betas(bits):
     s.new_gradients(1e-4)
     s.opt.step(s.grads)
     check_step(s, before, states, 2, s.states())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_places_past_32_bits(bits):
+    """One parameter of 2^32 and some values, zeros but for the last: their moves, states and random numbers are those of their own places. (A code may fall to the other side of the point that
+    decides where a value lies within fp32's error of it: of 1000 values 2^-18 each, so one at the most.)"""
+    first, n = 1 << 32, (1 << 32) + 1000
+    rng = np.random.default_rng(17)
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    p[first:], g[first:] = torch.from_numpy(rng.standard_normal(1000) * 0.05).cuda().bfloat16(), torch.from_numpy(rng.standard_normal(1000) * 1e-2).cuda().bfloat16()
+    before, grad = (np.concatenate([host(t[first:]), np.zeros(24)]) for t in (p, g))
+    opt = tn.AdamW([p], lr=LR, betas=BETAS, eps=EPS, weight_decay=DECAY, state_bits=bits, seed=77)
+    norm = float(opt.step([g], max_norm=0.1))
+    exact = np.sqrt((grad ** 2).sum())
+    assert abs(norm - exact) <= 2.0 ** -23 * exact
+    want, m, v = O.step(before, grad, 0.0, 0.0, 1, LR, *BETAS, EPS, DECAY, 0.1 / norm, O.least_root(*BETAS) if bits == 8 else 0.0)
+    s = opt.state_dict()
+    off = 2.0 ** -22 * np.abs(before) + 2.0 ** -18 * LR
+    assert (np.abs(host(s["master"][first:]) - want) <= off).all() and torch.equal(s["master"][first:first + 1000].bfloat16(), p[first:])
+    assert not bool(p[:first].any()) and not bool(s["master"][:first].any())
+    if bits == 32:
+        assert (np.abs(host(s["first"][first:]) - m) <= 2.0 ** -22 * np.abs(m)).all() and (np.abs(host(s["second"][first:]) - v) <= 2.0 ** -21 * v).all()
+        return
+    h = O.hash_of(77, 1, first + np.arange(1024))
+    for key, value, bits16 in (("first", m, h & np.uint64(0xFFFF)), ("second", np.sqrt(v), h >> np.uint64(16))):
+        codes, e = O.quantize(value, bits16)
+        assert np.array_equal(exponents(s[key + "_scales"][first // 128:]), e) and (host(s[key][first:]) != codes).sum() <= 1
