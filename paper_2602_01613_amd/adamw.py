@@ -147,12 +147,17 @@ class AdamW:
         """Masters from the parameters as they are: one launch on the current stream, in its place among the steps. Captured steps stay
         valid, and read the new masters."""
         self._open()
+        self._in_place()
         _check(_lib.tn_adamw_reset_master(self._handle, _stream(self._gpu)), "tn_adamw_reset_master")
 
     def _open(self) -> None:
         if self._handle is None:
             raise RuntimeError("optimizer was closed")
         _here("the optimizer", self._gpu)
+
+    def _in_place(self) -> None:
+        if [p.data_ptr() for p in self.params] != self._param_pointers:
+            raise RuntimeError("a parameter's memory is not where it was when the optimizer was made")
 
     def _gradients(self, grads: Sequence[torch.Tensor]):
         self._open()
@@ -206,8 +211,7 @@ class AdamW:
         max_norm. Where it is not finite nothing changes. Parameters count as modified in place for autograd, as by torch's own optimizers (a replayed
         step cannot say so)."""
         pointers, codes = self._gradients(grads)
-        if [p.data_ptr() for p in self.params] != self._param_pointers:
-            raise RuntimeError("a parameter's memory is not where it was when the optimizer was made")
+        self._in_place()
         rate, rate_ptr = self.lr, None
         if isinstance(lr, torch.Tensor):
             rate_ptr = self._scalar("lr", lr).data_ptr()

@@ -263,3 +263,18 @@ def test_a_given_norm_tensor_counts_as_written(monkeypatch):
     out = on_gpu(torch.zeros(()), 0)
     assert opt.gradient_norm([on_gpu(torch.zeros(5), 0)], out=out) is out
     assert [c[0] for c in calls] == ["tn_adamw_gradient_norm"] and out._version == 1
+
+
+def test_a_parameter_whose_memory_moved_is_refused(monkeypatch):
+    """The handle has the addresses of the parameters as they were: neither a step nor reset_master() may go there."""
+    from fp8_util import on_gpu
+    opt, calls = _optimizer(monkeypatch, [on_gpu(torch.zeros(5, dtype=torch.bfloat16), 0)])
+    grads = [on_gpu(torch.zeros(5), 0)]
+    opt.step(grads)
+    opt.reset_master()
+    assert [c[0] for c in calls] == ["tn_adamw_step", "tn_adamw_reset_master"]
+    opt.params[0] = on_gpu(torch.zeros(5, dtype=torch.bfloat16), 0)
+    for call in (lambda: opt.step(grads), opt.reset_master):
+        with pytest.raises(RuntimeError, match="not where it was"):
+            call()
+    assert len(calls) == 2
